@@ -1,6 +1,10 @@
 /*
  * la.h -- C ABI of the MI355X (gfx950) linear-attention library.
  *
+ * The attention comes first; the operators around it (gated recurrences, rows in 8 bits, the norm with
+ * the residual's addition) have their own conventions about shapes and alignment at the end, and
+ * share the rest with it: caller-owned buffers, streams, errors, no written buffer over another.
+ *
  * Linear attention with kernel f(x) = a + b*x (Sec. 2.2): for every (batch,
  * head) slice with rows q_i, k_i, v_i in R^D, i = 0..N-1,
  *
@@ -73,7 +77,9 @@ typedef enum la_status {
 
 typedef enum la_dtype {
     LA_F32 = 0,
-    LA_BF16 = 1
+    LA_BF16 = 1,
+    LA_E4M3 = 2,  /* 8-bit rows (la_pack_rows); no type of the attention's tensors */
+    LA_I8 = 3     /* the same with integers                                        */
 } la_dtype;
 
 struct la_trace; /* per-kernel timing hook, defined further down */
@@ -384,6 +390,123 @@ LA_API la_status la_backward_traced(const void *Q, const void *K, const void *V,
                       float a, float b, int causal, la_dtype dt,
                       void *workspace, size_t workspace_bytes, void *hip_stream,
                       la_trace *trace);
+
+/*
+ * Gated linear recurrence: the recurrence of App. B.1 with a gate per row and channel (the form that
+ * Table 3's gated rows share), on a vector state.  For each of B sequences of N rows with C channels
+ *
+ *     h_t = f_t h_{t-1} + u_t          (element-wise, t = 0 .. N-1, h_{-1} = h0)
+ *     LA_GATE_VALUE:    f_t = g_t,             u_t = x_t
+ *     LA_GATE_SIGMOID:  f_t = 1/(1+exp(-g_t)), u_t = (1 - f_t) x_t
+ *
+ * and backward, d_t being the gradient that reaches h_t from its own output and from all later rows,
+ *
+ *     d_t = dh_t + f_{t+1} d_{t+1}  (d_{N-1} = dh_{N-1} + dlast),   dh0 = f_0 d_0
+ *     LA_GATE_VALUE:    dx_t = d_t,            dg_t = d_t h_{t-1}
+ *     LA_GATE_SIGMOID:  dx_t = (1 - f_t) d_t,  dg_t = d_t (h_{t-1} - x_t) f_t (1 - f_t)
+ *
+ * The sequence is cut into segments that run in parallel, as in the attention's passes: what a segment
+ * does to a state is the product of its gates and its own sum.  States and sums are float32; h is
+ * stored in the tensors' type, and the backward pass goes by the stored h.
+ *
+ *   X, Gate, Hs, dHs, dX, dGate: [B, N, C] of `dt`, dense, C contiguous.  A head layout [B, H, N, D]
+ *       is B*H sequences of D channels.  Addresses are those of elements: no further alignment.
+ *   h0, last, dlast, dh0: [B, C] float32.  h0 NULL: zeros; last (the state after the last row) NULL:
+ *       not wanted; dlast NULL: zeros; dh0 NULL: not wanted.
+ *   lengths: NULL, or B ints on the device.  Rows from lengths[b] on are padding: they are not read,
+ *       every output is zero there, and `last` is the state before them (a length of 0 or less leaves
+ *       h0, one of N or more is N).
+ *   workspace: at least la_recurrence_workspace_bytes(..., is_backward) bytes, 256-byte aligned; NULL
+ *       where that is 0.  Nothing in it has to start at zero.
+ * A gate of zero (LA_GATE_SIGMOID: -infinity) starts anew: packed documents need no lengths.  The product
+ * of a run of gates has to be a float (gates of magnitude up to 1 are); an infinity or a NaN spoils its
+ * channel from its row on (backward: up to it), whatever the gates after it.
+ * Limits: B, N, C >= 1, B*N*C < 2^40, B * ceil(C / 64) < 2^23.
+ *
+ * la_recurrence_step appends T rows to a carried state, [B, C] float32, and updates it in place: the
+ * form for single tokens.  No workspace; rows are walked one after another, T is meant to be small.
+ * Calls that share a state must not overlap in time.
+ * Error behaviour as for la_forward; an unknown gate is LA_ERR_UNSUPPORTED.
+ */
+typedef enum la_gate {
+    LA_GATE_VALUE = 0,
+    LA_GATE_SIGMOID = 1
+} la_gate;
+
+LA_API size_t la_recurrence_workspace_bytes(int B, int N, int C, la_dtype dt, int is_backward);
+
+LA_API la_status la_recurrence_forward(const void *X, const void *Gate, const float *h0,
+                     void *Hs, float *last, const int *lengths,
+                     int B, int N, int C, la_gate gate, la_dtype dt,
+                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+LA_API la_status la_recurrence_backward(const void *X, const void *Gate, const float *h0,
+                      const void *Hs, const void *dHs, const float *dlast,
+                      void *dX, void *dGate, float *dh0, const int *lengths,
+                      int B, int N, int C, la_gate gate, la_dtype dt,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
+
+LA_API la_status la_recurrence_step(const void *X, const void *Gate, void *Hs, float *state,
+                     int B, int T, int C, la_gate gate, la_dtype dt, void *hip_stream);
+
+/*
+ * Rows in 8 bits: groups of 32 neighbours of a row (the last group of a row may be shorter) share a
+ * power of two, kept as one byte e that stands for 2^(e - 127): the block format of the OCP
+ * microscaling (MX) specification, which the matrix cores of gfx950 read as it stands.
+ *     LA_E4M3: codes are OCP e4m3 numbers;        the least power with  max |x| <= 448    2^(e - 127)
+ *     LA_I8:   codes are integers, 64ths of the power; the least with  max |x| <= 127/64 2^(e - 127)
+ * Elements are rounded to nearest, ties to even; e is held to 0 .. 254.  Every finite value that the
+ * codes stand for is a bfloat16 number, so that unpacking rounds nothing (below 2^-126 it may; with
+ * LA_E4M3 magnitudes from 1.9375 2^127 on round to 2^128 and come back as infinities).  A group with
+ * an infinity or a NaN gets e = 255 and comes back as NaN.
+ *
+ *   la_pack_rows:   X [rows, C] of `dt` (LA_F32 / LA_BF16) -> codes [rows, C], scales
+ *                   [rows, ceil(C / 32)] bytes
+ *   la_unpack_rows: the way back.
+ * One byte and 1/32 an element instead of two or four: what a backward pass keeps of a forward pass
+ * where memory is short (la_rmsnorm_backward reads the codes themselves).
+ * Addresses are those of elements.  Limits: rows, C >= 1, rows * C < 2^40.
+ */
+LA_API la_status la_pack_rows(const void *X, void *codes, void *scales, size_t rows, int C,
+                     la_dtype dt, la_dtype code, void *hip_stream);
+
+LA_API la_status la_unpack_rows(const void *codes, const void *scales, void *X, size_t rows, int C,
+                     la_dtype code, la_dtype dt, void *hip_stream);
+
+/*
+ * Root-mean-square norm of rows, with the residual's addition in front of it:
+ *
+ *     s = x + r (rounded to `dt`, as it is stored),  rstd = 1 / sqrt(mean(s^2) + eps),
+ *     y = w s rstd
+ * and backward, with n = s rstd and the gradients dy of y and ds of s (where s has other readers, as
+ * a residual stream has)
+ *     dx = dr = rstd (w dy - n mean(w dy n)) + ds,   dw = sum over the rows of dy n.
+ *
+ *   X, R, S, dY, dS, dX: [rows, C] of `dt` (LA_F32 / LA_BF16); W: [C] of `wt`, LA_F32 or `dt`.
+ *   R NULL: no residual, s is x; S must then be NULL too.  S may be R itself (updated in place).
+ *   W NULL: ones.  dS NULL: zeros.  dW: [C] float32, or NULL where it is not wanted (or W is NULL).
+ *   Y: [rows, C] of `yt`: `dt`, or LA_E4M3 / LA_I8, the codes of la_pack_rows with Yscale for their
+ *       powers (NULL otherwise): what a matrix product on 8-bit operands takes.
+ *   Kept, Kscale: NULL, or s in 8 bits of type `kt` for the backward pass, in the same pass over the rows.
+ *   rstd: [rows] float32, or NULL where no backward pass follows.
+ *   la_rmsnorm_backward: `st` is the type of S: `dt`, with Sscale NULL, or LA_E4M3 / LA_I8 (Kept,
+ *       Kscale of the forward call), whose values then stand for s.
+ *   workspace (only where dW is wanted): at least la_rmsnorm_workspace_bytes(rows, C) bytes, 256-byte
+ *       aligned.
+ * Sums are float32, those of dW in a fixed order.  The mean square of a row has to be a float.
+ * Addresses are those of elements.  Limits: rows >= 1, 1 <= C <= 16384, rows * C < 2^40.
+ */
+LA_API size_t la_rmsnorm_workspace_bytes(size_t rows, int C);
+
+LA_API la_status la_rmsnorm_forward(const void *X, const void *R, const void *W,
+                     void *Y, void *Yscale, void *S, void *Kept, void *Kscale, float *rstd,
+                     size_t rows, int C, float eps,
+                     la_dtype dt, la_dtype wt, la_dtype yt, la_dtype kt, void *hip_stream);
+
+LA_API la_status la_rmsnorm_backward(const void *S, const void *Sscale, const void *W, const float *rstd,
+                      const void *dY, const void *dS, void *dX, float *dW,
+                      size_t rows, int C, la_dtype dt, la_dtype wt, la_dtype st,
+                      void *workspace, size_t workspace_bytes, void *hip_stream);
 
 #ifdef __cplusplus
 }

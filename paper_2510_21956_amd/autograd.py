@@ -8,8 +8,13 @@ native code (binding.attention).  Every arithmetic step runs in the HIP library;
 Gradients are with respect to the Q, K, V handed in; with ``normalize_qk`` the rows of Q and
 K are scaled to unit length inside the kernels (Sec. 3.3) and the gradients are those for the
 raw rows.  a and b are constants.
+
+The operators around the attention follow below it in the same manner: gated_recurrence, rms_norm, and
+rows in 8 bits (pack_rows, unpack_rows, rms_norm_quantised, the ``checkpoint`` of linear_attention and
+rms_norm).
 """
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding as _b
 
@@ -57,10 +62,191 @@ def python_backward(Q, K, V, O, G, dO, saved, a, b, causal, normalize_qk):
     return dQ, dK, dV
 
 
-def linear_attention(Q, K, V, a=1.0, b=0.5, causal=True, normalize_qk=False):
+class CheckpointedAttentionFunction(torch.autograd.Function):
+    """The same with Q, K, V kept in 8 bits and nothing else: the backward pass unpacks them, runs the
+    forward pass again on what they stand for, and returns the gradients there."""
+
+    @staticmethod
+    def forward(ctx, Q, K, V, a, b, causal, normalize_qk, code):
+        Q, K, V = Q.contiguous(), K.contiguous(), V.contiguous()
+        B, H, N, D = Q.shape
+        dt = _code(Q)
+        O = torch.empty_like(Q)
+        ws = _bytes(_b.la_workspace_bytes(B, H, N, D, dt, causal, 0), Q.device)
+        (_b.la_forward_qknorm if normalize_qk else _b.la_forward)(Q, K, V, O, None, a, b, causal, ws)
+        ctx.save_for_backward(*(t for x in (Q, K, V) for t in pack_rows(x, code)))
+        ctx.la_args = (float(a), float(b), bool(causal), bool(normalize_qk))
+        ctx.la_code, ctx.la_dtype = code, Q.dtype
+        return O
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dO):
+        kept, (a, b, causal, normalize_qk) = ctx.saved_tensors, ctx.la_args
+        Q, K, V = (unpack_rows(kept[i], kept[i + 1], ctx.la_code, ctx.la_dtype) for i in (0, 2, 4))
+        B, H, N, D = Q.shape
+        dt = _code(Q)
+        O, G = torch.empty_like(Q), torch.empty((B, H, N), dtype=torch.float32, device=Q.device)
+        ws = _bytes(_b.la_workspace_bytes(B, H, N, D, dt, causal, 0), Q.device)
+        ns = _b.la_saved_state_bytes(B, H, N, D, dt, causal)
+        saved = _bytes(ns, Q.device) if ns else None
+        fwd = _b.la_forward_qknorm_save if normalize_qk else _b.la_forward_save
+        fwd(Q, K, V, O, G, a, b, causal, ws, saved)
+        return (*python_backward(Q, K, V, O, G, dO, saved, a, b, causal, normalize_qk), None, None, None, None, None)
+
+
+def linear_attention(Q, K, V, a=1.0, b=0.5, causal=True, normalize_qk=False, checkpoint=None):
     """Differentiable linear attention on [B, H, N, D] float32 or bfloat16 device tensors;
-    ``normalize_qk`` scales the rows of Q and K to unit length inside the kernels (D <= 128)."""
+    ``normalize_qk`` scales the rows of Q and K to unit length inside the kernels (D <= 128).
+
+    ``checkpoint`` "e4m3" or "int8" keeps Q, K, V for the backward pass in 8 bits (3.1 bytes an element of Q
+    instead of 8 in bfloat16, 16 in float32; la_pack_rows of include/la.h): the gradients are then those at the
+    values that the 8 bits stand for, and the backward pass runs the forward pass again."""
+    if checkpoint is not None:
+        code = _b.eight_bit_code(checkpoint)
+        if Q.shape != K.shape or Q.shape != V.shape:
+            raise ValueError("shape mismatch")
+        return CheckpointedAttentionFunction.apply(Q, K, V, a, b, causal, normalize_qk, code)
     O = _b.attention(Q, K, V, a, b, causal, normalize_qk)
     if O is not None:
         return O
     return LinearAttentionFunction.apply(Q, K, V, a, b, causal, normalize_qk)
+
+
+def pack_rows(x, code):
+    """x [..., C] in 8 bits: codes (float8_e4m3fn or int8) and the powers of two of 32 neighbours
+    (float8_e8m0fnu); ``code`` "e4m3", "int8", LA_E4M3 or LA_I8.  Not differentiable."""
+    code = _b.eight_bit_code(code) if isinstance(code, str) else code
+    x = x.detach().contiguous()
+    codes, scales = _eight_bits(x, code)
+    _b.la_pack_rows(x, codes, scales, code)
+    return codes, scales
+
+
+def unpack_rows(codes, scales, code, dtype):
+    """The values that pack_rows' codes stand for, as ``dtype`` (float32 or bfloat16)."""
+    code = _b.eight_bit_code(code) if isinstance(code, str) else code
+    codes, scales = codes.contiguous(), scales.contiguous()
+    x = torch.empty(codes.shape, dtype=dtype, device=codes.device)
+    _b.la_unpack_rows(codes, scales, x, code)
+    return x
+
+
+def _eight_bits(x, code):
+    """Room for x's codes and powers."""
+    kind = torch.float8_e4m3fn if code == _b.LA_E4M3 else torch.int8
+    groups = (*x.shape[:-1], -(-x.shape[-1] // _b.LA_GROUP))
+    return (torch.empty(x.shape, dtype=kind, device=x.device),
+            torch.empty(groups, dtype=torch.float8_e8m0fnu, device=x.device))
+
+
+_GATES = {"value": _b.LA_GATE_VALUE, "sigmoid": _b.LA_GATE_SIGMOID}
+
+
+class GatedRecurrenceFunction(torch.autograd.Function):
+    """h_t = f_t h_{t-1} + u_t (la_recurrence_forward); x, gates: [..., N, C] device tensors."""
+
+    @staticmethod
+    def forward(ctx, x, gates, h0, lengths, gate):
+        x, gates = x.contiguous(), gates.contiguous()
+        h0 = h0 if h0 is None else h0.contiguous()
+        lengths = lengths if lengths is None else lengths.contiguous()
+        h = torch.empty_like(x)
+        last = torch.empty((*x.shape[:-2], x.shape[-1]), dtype=torch.float32, device=x.device)
+        _b.la_recurrence_forward(x, gates, h0, h, last, lengths, gate, _recurrence_room(x, 0))
+        ctx.save_for_backward(x, gates, h0, h, lengths)
+        ctx.la_gate = gate
+        ctx.set_materialize_grads(False)
+        return h, last
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dh, dlast):
+        x, gates, h0, h, lengths = ctx.saved_tensors
+        dh = torch.zeros_like(x) if dh is None else dh.contiguous()
+        dlast = dlast if dlast is None else dlast.contiguous()
+        dx, dgates = torch.empty_like(x), torch.empty_like(x)
+        dh0 = torch.empty_like(h0) if ctx.needs_input_grad[2] else None
+        _b.la_recurrence_backward(x, gates, h0, h, dh, dlast, dx, dgates, dh0, lengths, ctx.la_gate,
+                                  _recurrence_room(x, 1))
+        return dx, dgates, dh0, None, None
+
+
+def _recurrence_room(x, is_backward):
+    N, C = x.shape[-2:]
+    n = _b.la_recurrence_workspace_bytes(x.numel() // (N * C) if x.numel() else 0, N, C, _code(x), is_backward)
+    return _bytes(n, x.device) if n else None
+
+
+def gated_recurrence(x, gates, h0=None, lengths=None, gate="sigmoid"):
+    """Differentiable gated linear recurrence along the second to last dimension of x, gates [..., N, C]
+    (float32 or bfloat16 device tensors): h_t = f_t h_{t-1} + u_t with
+
+      gate "sigmoid":  f_t = sigmoid(gates_t), u_t = (1 - f_t) x_t;   gate "value":  f_t = gates_t, u_t = x_t.
+
+    h0 [..., C] float32: the state before the first row (None: zeros).  lengths [...] int32: rows from there
+    on are padding, zero in every output.  Returns h like x and the state after the last row, [..., C] float32,
+    from which la_recurrence_step goes on."""
+    if gate not in _GATES:
+        raise ValueError("gates are %s, got %r" % (" and ".join(map(repr, _GATES)), gate))
+    return GatedRecurrenceFunction.apply(x, gates, h0, lengths, _GATES[gate])
+
+
+class RmsNormFunction(torch.autograd.Function):
+    """y = w s rstd, s = x + residual (la_rmsnorm_forward); x: [..., C] device tensors."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps, code):
+        x = x.contiguous()
+        residual = residual if residual is None else residual.contiguous()
+        weight = weight if weight is None else weight.contiguous()
+        y = torch.empty_like(x)
+        total = None if residual is None else torch.empty_like(x)
+        rstd = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+        kept, kscales = (None, None) if code is None else _eight_bits(x, code)
+        _b.la_rmsnorm_forward(x, residual, weight, y, None, total, kept, kscales, rstd, eps, None, code)
+        ctx.save_for_backward((x if total is None else total) if code is None else kept, kscales, weight, rstd)
+        ctx.la_code = code
+        ctx.set_materialize_grads(False)
+        return y, total
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dtotal):
+        total, scales, weight, rstd = ctx.saved_tensors
+        if dy is None:  # the sum alone was used
+            return dtotal, dtotal if ctx.needs_input_grad[1] else None, None, None, None
+        dy = dy.contiguous()
+        dtotal = dtotal if dtotal is None else dtotal.contiguous()
+        dx = torch.empty_like(dy)
+        dw = ws = None
+        if ctx.needs_input_grad[2]:
+            C = dy.shape[-1]
+            dw = torch.empty(C, dtype=torch.float32, device=dy.device)
+            ws = _bytes(_b.la_rmsnorm_workspace_bytes(dy.numel() // C, C), dy.device)
+        _b.la_rmsnorm_backward(total, scales, weight, rstd, dy, dtotal, dx, dw, ws, ctx.la_code)
+        return dx, dx if ctx.needs_input_grad[1] else None, dw if dw is None else dw.to(weight.dtype), None, None
+
+
+def rms_norm(x, weight=None, residual=None, eps=1e-6, checkpoint=None):
+    """Differentiable root-mean-square norm of the rows of x [..., C] (float32 or bfloat16 device tensors),
+    with ``residual`` added first: s = x + residual, y = weight s / sqrt(mean(s^2) + eps); weight [C] float32
+    or x's type (None: ones).  Returns y, or (y, s) where there is a residual.
+
+    ``checkpoint`` "e4m3" or "int8" keeps s in 8 bits for the backward pass, which then goes by those."""
+    code = None if checkpoint is None else _b.eight_bit_code(checkpoint)
+    y, total = RmsNormFunction.apply(x, residual, weight, float(eps), code)
+    return y if residual is None else (y, total)
+
+
+def rms_norm_quantised(x, weight=None, residual=None, eps=1e-6, code="e4m3"):
+    """rms_norm with y in 8 bits, for a matrix product on 8-bit operands: codes like x (float8_e4m3fn or
+    int8) and scales [..., ceil(C / 32)] (float8_e8m0fnu), and s where there is a residual.  Not differentiable."""
+    code = _b.eight_bit_code(code)
+    x = x.detach().contiguous()
+    residual = residual if residual is None else residual.detach().contiguous()
+    weight = weight if weight is None else weight.detach().contiguous()
+    codes, scales = _eight_bits(x, code)
+    total = None if residual is None else torch.empty_like(x)
+    _b.la_rmsnorm_forward(x, residual, weight, codes, scales, total, None, None, None, eps, code)
+    return (codes, scales) if residual is None else (codes, scales, total)

@@ -20,6 +20,11 @@ _native = None  # the module of _marshal.so once the library is loaded
 
 LA_F32 = 0
 LA_BF16 = 1
+LA_E4M3 = 2
+LA_I8 = 3
+
+LA_GATE_VALUE = 0
+LA_GATE_SIGMOID = 1
 
 LA_MAX_TRACE = 8
 
@@ -27,7 +32,10 @@ EXPORTS = ("la_version", "la_status_string", "la_workspace_bytes", "la_forward",
            "la_forward_traced", "la_backward_traced", "la_saved_state_bytes", "la_forward_save",
            "la_backward_saved", "la_debug_override", "la_forward_static", "la_decode_state_bytes",
            "la_decode_step", "la_decode_prefill", "la_backward_ab", "la_forward_qknorm",
-           "la_backward_qknorm", "la_forward_qknorm_save", "la_backward_qknorm_saved")
+           "la_backward_qknorm", "la_forward_qknorm_save", "la_backward_qknorm_saved",
+           "la_recurrence_workspace_bytes", "la_recurrence_forward", "la_recurrence_backward",
+           "la_recurrence_step", "la_pack_rows", "la_unpack_rows", "la_rmsnorm_workspace_bytes",
+           "la_rmsnorm_forward", "la_rmsnorm_backward")
 
 
 class la_trace(ctypes.Structure):
@@ -99,6 +107,24 @@ def load_library():
     lib.la_backward_qknorm_saved.argtypes = lib.la_backward_saved.argtypes
     lib.la_backward_ab.restype = i
     lib.la_backward_ab.argtypes = [vp] * 7 + [i, i, i, i, f, f, i, i, vp, sz, vp]
+    lib.la_recurrence_workspace_bytes.restype = sz
+    lib.la_recurrence_workspace_bytes.argtypes = [i] * 5
+    lib.la_recurrence_forward.restype = i
+    lib.la_recurrence_forward.argtypes = [vp] * 6 + [i] * 5 + [vp, sz, vp]
+    lib.la_recurrence_backward.restype = i
+    lib.la_recurrence_backward.argtypes = [vp] * 10 + [i] * 5 + [vp, sz, vp]
+    lib.la_recurrence_step.restype = i
+    lib.la_recurrence_step.argtypes = [vp] * 4 + [i] * 5 + [vp]
+    lib.la_pack_rows.restype = i
+    lib.la_pack_rows.argtypes = [vp, vp, vp, sz, i, i, i, vp]
+    lib.la_unpack_rows.restype = i
+    lib.la_unpack_rows.argtypes = [vp, vp, vp, sz, i, i, i, vp]
+    lib.la_rmsnorm_workspace_bytes.restype = sz
+    lib.la_rmsnorm_workspace_bytes.argtypes = [sz, i]
+    lib.la_rmsnorm_forward.restype = i
+    lib.la_rmsnorm_forward.argtypes = [vp] * 9 + [sz, i, f, i, i, i, i, vp]
+    lib.la_rmsnorm_backward.restype = i
+    lib.la_rmsnorm_backward.argtypes = [vp] * 8 + [sz, i, i, i, i, vp, sz, vp]
     lib.la_debug_override.restype = None
     lib.la_debug_override.argtypes = [i, i]
     _lib = lib
@@ -469,3 +495,219 @@ def la_backward_qknorm_saved(Q, K, V, O, G, dO, dQ, dK, dV, a, b, causal, worksp
     """la_backward_qknorm_saved of include/la.h; ``saved`` as filled by la_forward_qknorm_save."""
     _backward(Q, K, V, O, G, dO, dQ, dK, dV, a, b, causal, workspace, saved, stream, trace,
               "qknorm_save")
+
+
+# ---- the operators around the attention ---------------------------------------------------------
+
+def _call(name, ref, stream, *args):
+    """Calls the entry point with the stream behind its arguments, on ref's device."""
+    f = getattr(load_library(), name)
+    index = ref.get_device()
+    if torch.cuda.current_device() == index:
+        rc = f(*args, _stream_ptr(stream, ref))
+    else:
+        with torch.cuda.device(index):
+            rc = f(*args, _stream_ptr(stream, ref))
+    if rc != 0:
+        raise LaError(rc, name)
+
+
+def _room(t):
+    return (None, 0) if t is None else (_ptr(t), t.numel() * t.element_size())
+
+
+def _like(ref, **ts):
+    """Every tensor given has ref's shape and type."""
+    for name, t in ts.items():
+        if t is None:
+            continue
+        if t.shape != ref.shape:
+            raise ValueError("%s must be %s, got %s" % (name, tuple(ref.shape), tuple(t.shape)))
+        if t.dtype != ref.dtype:
+            raise TypeError("%s must be %s, got %s" % (name, ref.dtype, t.dtype))
+
+
+def _needed(**ts):
+    for name, t in ts.items():
+        if t is None:
+            raise ValueError("%s is required" % name)
+
+
+def _real_code(t):
+    if t.dtype not in (torch.float32, torch.bfloat16):
+        raise TypeError("tensors must be float32 or bfloat16, got %s" % t.dtype)
+    return LA_F32 if t.dtype == torch.float32 else LA_BF16
+
+
+def la_recurrence_workspace_bytes(B, N, C, dt, is_backward):
+    return int(load_library().la_recurrence_workspace_bytes(B, N, C, dt, int(bool(is_backward))))
+
+
+def _sequences(x, **states):
+    """B, N, C of x [..., N, C]; states are float32 of one row a sequence."""
+    if x.dim() < 2:
+        raise ValueError("x must be [..., N, C]")
+    N, C = x.shape[-2:]
+    for name, t in states.items():
+        if t is not None and (t.shape != x.shape[:-2] + x.shape[-1:] or t.dtype != torch.float32):
+            raise ValueError("%s must be float32 %s" % (name, tuple(x.shape[:-2] + x.shape[-1:])))
+    return (x.numel() // (N * C) if x.numel() else 0), N, C
+
+
+def _lengths_ptr(lengths, x):
+    if lengths is None:
+        return None
+    if lengths.dtype != torch.int32 or lengths.shape != x.shape[:-2]:
+        raise ValueError("lengths must be int32 %s" % (tuple(x.shape[:-2]),))
+    return _ptr(lengths)
+
+
+def la_recurrence_forward(x, gates, h0, h, last, lengths, gate, workspace, stream=None):
+    """la_recurrence_forward of include/la.h: x, gates, h [..., N, C] float32 or bfloat16; h0, last
+    [..., C] float32 or None; lengths [...] int32 or None; gate LA_GATE_VALUE or LA_GATE_SIGMOID;
+    workspace: uint8 device tensor of la_recurrence_workspace_bytes(..., 0) bytes (None where that is 0)."""
+    _needed(x=x, gates=gates, h=h)
+    _check_tensors(x, gates, h0, h, last, lengths, workspace)
+    _like(x, gates=gates, h=h)
+    B, N, C = _sequences(x, h0=h0, last=last)
+    _call("la_recurrence_forward", x, stream, _ptr(x), _ptr(gates), _ptr(h0), _ptr(h), _ptr(last),
+          _lengths_ptr(lengths, x), B, N, C, int(gate), _real_code(x), *_room(workspace))
+
+
+def la_recurrence_backward(x, gates, h0, h, dh, dlast, dx, dgates, dh0, lengths, gate, workspace, stream=None):
+    """la_recurrence_backward of include/la.h (see la_recurrence_forward; dlast, dh0 [..., C] float32 or None)."""
+    _needed(x=x, gates=gates, h=h, dh=dh, dx=dx, dgates=dgates)
+    _check_tensors(x, gates, h0, h, dh, dlast, dx, dgates, dh0, lengths, workspace)
+    _like(x, gates=gates, h=h, dh=dh, dx=dx, dgates=dgates)
+    B, N, C = _sequences(x, h0=h0, dlast=dlast, dh0=dh0)
+    _call("la_recurrence_backward", x, stream, _ptr(x), _ptr(gates), _ptr(h0), _ptr(h), _ptr(dh), _ptr(dlast),
+          _ptr(dx), _ptr(dgates), _ptr(dh0), _lengths_ptr(lengths, x), B, N, C, int(gate), _real_code(x),
+          *_room(workspace))
+
+
+def la_recurrence_step(x, gates, h, state, gate, stream=None):
+    """la_recurrence_step of include/la.h: x, gates, h [..., T, C]; state [..., C] float32, updated in place."""
+    _needed(x=x, gates=gates, h=h, state=state)
+    _check_tensors(x, gates, h, state)
+    _like(x, gates=gates, h=h)
+    B, T, C = _sequences(x, state=state)
+    _call("la_recurrence_step", x, stream, _ptr(x), _ptr(gates), _ptr(h), _ptr(state), B, T, C, int(gate), _real_code(x))
+
+
+LA_GROUP = 32  # neighbours of a row that share a power of two
+_EIGHT = {"e4m3": LA_E4M3, "int8": LA_I8}
+
+
+def eight_bit_code(name):
+    """LA_E4M3 or LA_I8 from a type's name."""
+    if name not in _EIGHT:
+        raise ValueError("8-bit types are %s, got %r" % (" and ".join(map(repr, _EIGHT)), name))
+    return _EIGHT[name]
+
+
+def _eight(codes, scales, x, code, what):
+    """Checks codes like x and a power for every 32 elements of a row; both of one byte an element."""
+    if code not in (LA_E4M3, LA_I8):
+        raise ValueError("%s: the code is LA_E4M3 or LA_I8, got %r" % (what, code))
+    _needed(**{what + " codes": codes, what + " scales": scales})
+    if codes.shape != x.shape or codes.element_size() != 1:
+        raise ValueError("%s codes must be %s of one byte an element" % (what, tuple(x.shape)))
+    groups = x.shape[:-1] + (-(-x.shape[-1] // LA_GROUP),)
+    if scales.shape != groups or scales.element_size() != 1:
+        raise ValueError("%s scales must be %s of one byte an element" % (what, tuple(groups)))
+
+
+def _rows(x):
+    if x.dim() < 1:
+        raise ValueError("rows of [..., C] are needed")
+    C = x.shape[-1]
+    return (x.numel() // C if x.numel() else 0), C
+
+
+def la_pack_rows(x, codes, scales, code, stream=None):
+    """la_pack_rows of include/la.h: x [..., C] float32 or bfloat16 -> codes [..., C], scales
+    [..., ceil(C / 32)], any types of one byte; code LA_E4M3 or LA_I8."""
+    _needed(x=x)
+    _check_tensors(x, codes, scales)
+    _eight(codes, scales, x, code, "packed")
+    rows, C = _rows(x)
+    _call("la_pack_rows", x, stream, _ptr(x), _ptr(codes), _ptr(scales), rows, C, _real_code(x), int(code))
+
+
+def la_unpack_rows(codes, scales, x, code, stream=None):
+    """la_unpack_rows of include/la.h: the way back, into x."""
+    _needed(x=x)
+    _check_tensors(x, codes, scales)
+    _eight(codes, scales, x, code, "packed")
+    rows, C = _rows(x)
+    _call("la_unpack_rows", x, stream, _ptr(codes), _ptr(scales), _ptr(x), rows, C, int(code), _real_code(x))
+
+
+def la_rmsnorm_workspace_bytes(rows, C):
+    return int(load_library().la_rmsnorm_workspace_bytes(rows, C))
+
+
+def _weight_code(weight, x):
+    if weight is None:
+        return LA_F32
+    if weight.shape != x.shape[-1:]:
+        raise ValueError("the weight must be [%d], got %s" % (x.shape[-1], tuple(weight.shape)))
+    if weight.dtype not in (torch.float32, x.dtype):
+        raise TypeError("the weight must be float32 or %s, got %s" % (x.dtype, weight.dtype))
+    return LA_F32 if weight.dtype == torch.float32 else LA_BF16
+
+
+def _per_row(x, **ts):
+    for name, t in ts.items():
+        if t is not None and (t.shape != x.shape[:-1] or t.dtype != torch.float32):
+            raise ValueError("%s must be float32 %s" % (name, tuple(x.shape[:-1])))
+
+
+def la_rmsnorm_forward(x, residual, weight, y, yscales, total, kept, kscales, rstd, eps, ycode=None, kcode=None,
+                       stream=None):
+    """la_rmsnorm_forward of include/la.h: x, residual, total [..., C] float32 or bfloat16 (residual and
+    total together, or both None); weight [C] float32 or x's type, or None; y like x (yscales, ycode None)
+    or 8-bit codes; kept, kscales, kcode: the sum in 8 bits, or None; rstd [...] float32 or None."""
+    _needed(x=x, y=y)
+    _check_tensors(x, residual, weight, y, yscales, total, kept, kscales, rstd)
+    _like(x, residual=residual, total=total)
+    if (residual is None) != (total is None):
+        raise ValueError("residual and total go together")
+    dt, wt = _real_code(x), _weight_code(weight, x)
+    if ycode is None:
+        _like(x, y=y)
+        if yscales is not None:
+            raise ValueError("yscales belong to 8-bit codes (ycode)")
+    else:
+        _eight(y, yscales, x, ycode, "y")
+    if kcode is not None:
+        _eight(kept, kscales, x, kcode, "kept")
+    elif kept is not None or kscales is not None:
+        raise ValueError("kept and kscales need kcode")
+    _per_row(x, rstd=rstd)
+    rows, C = _rows(x)
+    _call("la_rmsnorm_forward", x, stream, _ptr(x), _ptr(residual), _ptr(weight), _ptr(y), _ptr(yscales), _ptr(total),
+          _ptr(kept), _ptr(kscales), _ptr(rstd), rows, C, float(eps), dt, wt, dt if ycode is None else int(ycode),
+          LA_E4M3 if kcode is None else int(kcode))
+
+
+def la_rmsnorm_backward(total, scales, weight, rstd, dy, dtotal, dx, dweight, workspace, code=None, stream=None):
+    """la_rmsnorm_backward of include/la.h: total like dy (scales, code None) or the 8-bit codes that
+    la_rmsnorm_forward kept; dy, dtotal (or None), dx [..., C]; dweight [C] float32 or None; workspace: uint8
+    device tensor of la_rmsnorm_workspace_bytes(rows, C) bytes where dweight is given."""
+    _needed(total=total, rstd=rstd, dy=dy, dx=dx)
+    _check_tensors(dy, total, scales, weight, rstd, dtotal, dx, dweight, workspace)
+    _like(dy, dtotal=dtotal, dx=dx)
+    if code is None:
+        _like(dy, total=total)
+        if scales is not None:
+            raise ValueError("scales belong to 8-bit codes (code)")
+    else:
+        _eight(total, scales, dy, code, "total")
+    dt, wt = _real_code(dy), _weight_code(weight, dy)
+    if dweight is not None and (weight is None or dweight.shape != weight.shape or dweight.dtype != torch.float32):
+        raise ValueError("dweight must be float32, of the weight's shape")
+    _per_row(dy, rstd=rstd)
+    rows, C = _rows(dy)
+    _call("la_rmsnorm_backward", dy, stream, _ptr(total), _ptr(scales), _ptr(weight), _ptr(rstd), _ptr(dy), _ptr(dtotal),
+          _ptr(dx), _ptr(dweight), rows, C, dt, wt, dt if code is None else int(code), *_room(workspace))

@@ -1,6 +1,7 @@
 // C ABI entry points: argument validation, segment plan, dispatch.
 #include <atomic>
 
+#include "la_checks.h"
 #include "la_common.h"
 
 namespace la {
@@ -13,8 +14,6 @@ static __device__ __align__(256) unsigned char scratch[LA_STATIC_SCRATCH_BYTES];
 // Test / profiling override (la_debug_override): 0 = automatic.
 static std::atomic<int> g_seg_len_override{0};
 static std::atomic<int> g_force_generic{0};
-
-static size_t round_up(size_t x, size_t m) { return (x + m - 1) / m * m; }
 
 static bool supported_d(int D) { return D == 16 || D == 32 || D == 64 || D == 128 || D == 256; }
 
@@ -166,28 +165,6 @@ static bool grid_ok(int B, int H, const Plan &pl)
 }
 
 static bool aligned16(const void *p) { return (((uintptr_t)p) & 15u) == 0; }
-
-struct Range {
-    const void *p;
-    size_t bytes;
-};
-static bool overlap(const Range &x, const Range &y)
-{
-    if (!x.p || !y.p || !x.bytes || !y.bytes) return false;
-    const uintptr_t a0 = (uintptr_t)x.p, a1 = a0 + x.bytes, b0 = (uintptr_t)y.p, b1 = b0 + y.bytes;
-    return a0 < b1 && b0 < a1;
-}
-// No written buffer (outs) may overlap any other buffer of the call.
-static bool any_alias(const Range *ins, int nin, const Range *outs, int nout)
-{
-    for (int i = 0; i < nout; ++i) {
-        for (int j = 0; j < nin; ++j)
-            if (overlap(outs[i], ins[j])) return true;
-        for (int j = i + 1; j < nout; ++j)
-            if (overlap(outs[i], outs[j])) return true;
-    }
-    return false;
-}
 
 // D = 16 on the tiles of D = 32: the forward and backward passes (no hand-over buffer).
 static bool use_padded(const Problem &pr)

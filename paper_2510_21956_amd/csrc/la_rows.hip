@@ -1,0 +1,410 @@
+// Root-mean-square norm of rows with the residual's addition, its backward pass, and rows in 8 bits.
+//
+// All of it is one pass over the rows, bound by HBM: a row stays in the registers of the lanes that share it
+// (8 to 1024 of them, eight neighbouring elements to a lane and step), from the sum of its squares to the
+// normalised row; nothing is read twice.
+#include "la_checks.h"
+#include "la_eight.h"
+
+namespace la {
+namespace {
+
+// L lanes share a row and take K steps of 8 L elements each; a workgroup has max(L, 256) lanes.
+template <int L>
+struct Share {
+    static constexpr int NT = L > 256 ? L : 256, ROWS = NT / L, WAVES = L / 64;
+};
+
+// Sums over the lanes that share a row, in every one of them.
+template <int L, int M>
+__device__ __forceinline__ void row_sums(float (&s)[M], float *lds)
+{
+#pragma unroll
+    for (int m = (L < 64 ? L : 64) / 2; m >= 1; m >>= 1)
+#pragma unroll
+        for (int j = 0; j < M; ++j) s[j] += __shfl_xor(s[j], m);
+    if constexpr (L > 64) {  // NT / L rows of L / 64 waves each
+        const int wave = threadIdx.x / 64;
+        block_sync();  // the shares of the row before have been read
+        if (threadIdx.x % 64 == 0)
+#pragma unroll
+            for (int j = 0; j < M; ++j) lds[wave * M + j] = s[j];
+        block_sync();
+        const int first = wave / (L / 64) * (L / 64);
+#pragma unroll
+        for (int j = 0; j < M; ++j) {
+            float t = 0.f;
+#pragma unroll
+            for (int v = 0; v < L / 64; ++v) t += lds[(first + v) * M + j];
+            s[j] = t;
+        }
+    }
+}
+
+struct Norm {
+    const void *X, *R, *W;
+    void *Y, *S;
+    uint8_t *Yp, *K, *Kp;
+    float *rstd;
+    size_t rows;
+    int C;
+    float eps;
+    int yt, kt;  // la_dtype
+};
+
+template <typename T, typename TW, int L, int K>
+__global__ void __launch_bounds__(Share<L>::NT) k_norm(Norm a)
+{
+    __shared__ float lds[Share<L>::NT / 64];
+    const int lane = threadIdx.x % L, C = a.C, G = (C + kGroup - 1) / kGroup;
+    const size_t step = (size_t)gridDim.x * Share<L>::ROWS;
+    for (size_t base = (size_t)blockIdx.x * Share<L>::ROWS; base < a.rows; base += step) {
+        const size_t row = base + threadIdx.x / L;
+        const bool here = row < a.rows;
+        const size_t at = (here ? row : 0) * C;
+        Eight t[K];
+        float ss[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * L + lane) * 8, valid = here ? C - c : 0;
+            t[k] = load8((const T *)a.X + at + c, valid);
+            if (a.R) {
+                const Eight r = load8((const T *)a.R + at + c, valid);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {  // as it is stored: what the backward pass will read
+                    T s[1];
+                    store_elem(s, 0, t[k].x[j] + r.x[j]);
+                    t[k].x[j] = load_elem(s, 0);
+                }
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ss[0] += t[k].x[j] * t[k].x[j];
+        }
+        row_sums<L>(ss, lds);
+        const float rstd = 1.f / sqrtf(ss[0] / (float)C + a.eps);
+        if (here && lane == 0 && a.rstd) a.rstd[row] = rstd;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * L + lane) * 8, valid = here ? C - c : 0;
+            if (a.S) store8((T *)a.S + at + c, t[k], valid);
+            if (a.K) pack8(t[k], a.K + at, a.Kp + (here ? row : 0) * G, c, valid, a.kt == LA_I8);
+            Eight y = t[k];
+            if (a.W) {
+                const Eight w = load8((const TW *)a.W + c, valid);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y.x[j] = y.x[j] * rstd * w.x[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) y.x[j] *= rstd;
+            }
+            if (a.Yp) pack8(y, (uint8_t *)a.Y + at, a.Yp + (here ? row : 0) * G, c, valid, a.yt == LA_I8);
+            else store8((T *)a.Y + at + c, y, valid);
+        }
+    }
+}
+
+struct NormBack {
+    const void *S, *W, *dY, *dS;
+    const uint8_t *Sp;
+    const float *rstd;
+    void *dX;
+    float *parts;  // [gridDim.x, C] shares of dw
+    size_t rows;
+    int C, st;
+};
+
+template <typename T, typename TW, int L, int K>
+__global__ void __launch_bounds__(Share<L>::NT) k_norm_back(NormBack a)
+{
+    __shared__ float lds[Share<L>::NT / 64];
+    __shared__ float shares[Share<L>::ROWS > 1 ? Share<L>::NT * 8 * K : 1];
+    const int lane = threadIdx.x % L, C = a.C, G = (C + kGroup - 1) / kGroup;
+    const size_t step = (size_t)gridDim.x * Share<L>::ROWS;
+    Eight w[K], dw[K];
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        const int c = (k * L + lane) * 8;
+        if (a.W) w[k] = load8((const TW *)a.W + c, C - c);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (!a.W) w[k].x[j] = 1.f;
+            dw[k].x[j] = 0.f;
+        }
+    }
+    for (size_t base = (size_t)blockIdx.x * Share<L>::ROWS; base < a.rows; base += step) {
+        const size_t row = base + threadIdx.x / L;
+        const bool here = row < a.rows;
+        const size_t at = (here ? row : 0) * C;
+        const float rstd = here ? a.rstd[row] : 0.f;
+        Eight n[K], d[K];
+        float m[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * L + lane) * 8, valid = here ? C - c : 0;
+            if (a.Sp) {
+                const uint2 codes = load_codes((const uint8_t *)a.S + at + c, valid);
+                const int e = valid > 0 ? a.Sp[row * G + c / kGroup] : 127;
+                n[k] = values_of(codes, e, a.st == LA_I8);
+            } else n[k] = load8((const T *)a.S + at + c, valid);
+            d[k] = load8((const T *)a.dY + at + c, valid);
+        }
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                n[k].x[j] *= rstd;
+                dw[k].x[j] += d[k].x[j] * n[k].x[j];
+                d[k].x[j] *= w[k].x[j];
+                m[0] += d[k].x[j] * n[k].x[j];
+            }
+        row_sums<L>(m, lds);
+        const float mean = m[0] / (float)C;
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * L + lane) * 8, valid = here ? C - c : 0;
+            if (a.dS) {
+                const Eight s = load8((const T *)a.dS + at + c, valid);
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[k].x[j] = rstd * (d[k].x[j] - n[k].x[j] * mean) + s.x[j];
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) d[k].x[j] = rstd * (d[k].x[j] - n[k].x[j] * mean);
+            }
+            store8((T *)a.dX + at + c, d[k], valid);
+        }
+    }
+    if (!a.parts) return;
+    float *out = a.parts + (size_t)blockIdx.x * C;
+    if constexpr (Share<L>::ROWS > 1) {  // the workgroup's rows, in their order
+        constexpr int W8 = L * 8 * K;
+#pragma unroll
+        for (int k = 0; k < K; ++k)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) shares[threadIdx.x / L * W8 + (k * L + lane) * 8 + j] = dw[k].x[j];
+        block_sync();
+        for (int c = threadIdx.x; c < C; c += Share<L>::NT) {
+            float s = 0.f;
+#pragma unroll
+            for (int r = 0; r < Share<L>::ROWS; ++r) s += shares[r * W8 + c];
+            out[c] = s;
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            const int c = (k * L + lane) * 8;
+            store8(out + c, dw[k], C - c);
+        }
+    }
+}
+
+// dw from its shares: 64 channels a workgroup, sixteen runs of shares side by side.
+__global__ void __launch_bounds__(1024) k_norm_join(const float *parts, float *dW, int n, int C)
+{
+    __shared__ float lds[16][64];
+    const int lane = threadIdx.x % 64, run = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
+    const int per = (n + 15) / 16, end = min(n, (run + 1) * per);
+    float s = 0.f;
+    if (c < C)
+#pragma unroll 4
+        for (int i = run * per; i < end; ++i) s += parts[(size_t)i * C + c];
+    lds[run][lane] = s;
+    block_sync();
+    if (run == 0 && c < C) {
+        s = 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s += lds[r][lane];
+        dW[c] = s;
+    }
+}
+
+// Eight elements a lane; four lanes to a group, and as many to the last group of a row however short it is.
+template <typename T, bool PACK>
+__global__ void __launch_bounds__(256) k_rows8(const T *X, T *Xout, const uint8_t *codes, uint8_t *codes_out,
+                                               const uint8_t *powers, uint8_t *powers_out, size_t rows, int C, int ints)
+{
+    const int G = (C + kGroup - 1) / kGroup, lanes = G * 4;
+    const size_t total = rows * lanes, step = (size_t)gridDim.x * 256;
+    for (size_t base = (size_t)blockIdx.x * 256; base < total; base += step) {
+        const size_t i = base + threadIdx.x;
+        const bool here = i < total;
+        const size_t row = here ? i / lanes : 0;
+        const int c = here ? (int)(i - row * lanes) * 8 : 0, valid = here ? C - c : 0;
+        if constexpr (PACK) {
+            const Eight x = load8(X + row * C + c, valid);
+            pack8(x, codes_out + row * C, powers_out + row * G, c, valid, ints);
+        } else if (valid > 0) {
+            const Eight x = values_of(load_codes(codes + row * C + c, valid), powers[row * G + c / kGroup], ints);
+            store8(Xout + row * C + c, x, valid);
+        }
+    }
+}
+
+constexpr int kMostColumns = 16384;  // of the norm, whose rows stay in registers
+
+// Workgroups of the backward pass: two a compute unit at most, so that the shares of dw are few.
+int back_blocks(size_t groups) { return (int)(groups < 512 ? groups : 512); }
+int row_lanes(int C) { return C <= 64 ? 8 : C <= 128 ? 16 : C <= 256 ? 32 : C <= 2048 ? 64 : C <= 8192 ? 256 : 1024; }
+size_t row_groups(size_t rows, int C)
+{
+    const int L = row_lanes(C), per = L > 256 ? 1 : 256 / L;
+    return (rows + per - 1) / per;
+}
+
+// Calls f with the shape (L, K) that holds a row of C elements.
+template <int L, int K>
+struct Shape {
+    static constexpr int l = L, k = K;
+};
+template <typename F>
+void by_width(int C, F f)
+{
+    if (C <= 64) f(Shape<8, 1>());
+    else if (C <= 128) f(Shape<16, 1>());
+    else if (C <= 256) f(Shape<32, 1>());
+    else if (C <= 512) f(Shape<64, 1>());
+    else if (C <= 1024) f(Shape<64, 2>());
+    else if (C <= 2048) f(Shape<64, 4>());
+    else if (C <= 4096) f(Shape<256, 2>());
+    else if (C <= 8192) f(Shape<256, 4>());
+    else f(Shape<1024, 2>());
+}
+template <typename F>
+void by_types(la_dtype dt, la_dtype wt, F f)
+{
+    if (dt == LA_F32) f((float *)nullptr, (float *)nullptr);
+    else if (wt == LA_F32) f((bf16_t *)nullptr, (float *)nullptr);
+    else f((bf16_t *)nullptr, (bf16_t *)nullptr);
+}
+
+la_status check_rows(size_t rows, int C, int most)
+{
+    if (rows < 1 || C < 1) return LA_ERR_SHAPE;
+    if (C > most || (double)rows * C >= 1099511627776.0) return LA_ERR_SHAPE;  // 2^40
+    return LA_OK;
+}
+size_t powers_bytes(size_t rows, int C) { return rows * ((C + kGroup - 1) / kGroup); }
+la_status done() { return hipGetLastError() == hipSuccess ? LA_OK : LA_ERR_LAUNCH; }
+
+template <bool PACK>
+la_status rows8(const void *X, void *Xo, const void *codes, void *codes_o, const void *powers, void *powers_o,
+                size_t rows, int C, la_dtype dt, la_dtype code, hipStream_t st)
+{
+    const size_t lanes = powers_bytes(rows, C) * 4, blocks = (lanes + 255) / 256;
+    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384)), block(256);
+    if (dt == LA_F32)
+        k_rows8<float, PACK><<<grid, block, 0, st>>>((const float *)X, (float *)Xo, (const uint8_t *)codes, (uint8_t *)codes_o,
+                                                     (const uint8_t *)powers, (uint8_t *)powers_o, rows, C, code == LA_I8);
+    else
+        k_rows8<bf16_t, PACK><<<grid, block, 0, st>>>((const bf16_t *)X, (bf16_t *)Xo, (const uint8_t *)codes, (uint8_t *)codes_o,
+                                                      (const uint8_t *)powers, (uint8_t *)powers_o, rows, C, code == LA_I8);
+    return done();
+}
+
+}  // namespace
+}  // namespace la
+
+extern "C" {
+
+la_status la_pack_rows(const void *X, void *codes, void *scales, size_t rows, int C, la_dtype dt, la_dtype code,
+                       void *hip_stream)
+{
+    const la_status s = la::check_rows(rows, C, 2147483647 - 64);
+    if (s != LA_OK) return s;
+    if (!la::real_type(dt) || !la::eight_bits(code)) return LA_ERR_UNSUPPORTED;
+    if (!X || !codes || !scales) return LA_ERR_NULL;
+    if (!la::aligned_to(X, la::size_of(dt))) return LA_ERR_ALIGN;
+    const la::Range ins[] = {{X, rows * C * la::size_of(dt)}};
+    const la::Range outs[] = {{codes, rows * C}, {scales, la::powers_bytes(rows, C)}};
+    if (la::any_alias(ins, 1, outs, 2)) return LA_ERR_ALIAS;
+    if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
+    return la::rows8<true>(X, nullptr, nullptr, codes, nullptr, scales, rows, C, dt, code, (hipStream_t)hip_stream);
+}
+
+la_status la_unpack_rows(const void *codes, const void *scales, void *X, size_t rows, int C, la_dtype code,
+                         la_dtype dt, void *hip_stream)
+{
+    const la_status s = la::check_rows(rows, C, 2147483647 - 64);
+    if (s != LA_OK) return s;
+    if (!la::real_type(dt) || !la::eight_bits(code)) return LA_ERR_UNSUPPORTED;
+    if (!X || !codes || !scales) return LA_ERR_NULL;
+    if (!la::aligned_to(X, la::size_of(dt))) return LA_ERR_ALIGN;
+    const la::Range ins[] = {{codes, rows * C}, {scales, la::powers_bytes(rows, C)}};
+    const la::Range outs[] = {{X, rows * C * la::size_of(dt)}};
+    if (la::any_alias(ins, 2, outs, 1)) return LA_ERR_ALIAS;
+    if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
+    return la::rows8<false>(nullptr, X, codes, nullptr, scales, nullptr, rows, C, dt, code, (hipStream_t)hip_stream);
+}
+
+size_t la_rmsnorm_workspace_bytes(size_t rows, int C)
+{
+    if (la::check_rows(rows, C, la::kMostColumns) != LA_OK) return 0;
+    return la::round_up((size_t)la::back_blocks(la::row_groups(rows, C)) * C * 4, 256);
+}
+
+la_status la_rmsnorm_forward(const void *X, const void *R, const void *W, void *Y, void *Yscale, void *S, void *Kept,
+                             void *Kscale, float *rstd, size_t rows, int C, float eps, la_dtype dt, la_dtype wt,
+                             la_dtype yt, la_dtype kt, void *hip_stream)
+{
+    const la_status s = la::check_rows(rows, C, la::kMostColumns);
+    if (s != LA_OK) return s;
+    if (!la::real_type(dt) || (W && wt != LA_F32 && wt != dt)) return LA_ERR_UNSUPPORTED;
+    if ((yt != dt && !la::eight_bits(yt)) || (Kept && !la::eight_bits(kt))) return LA_ERR_UNSUPPORTED;
+    if (!X || !Y || (yt != dt) != (Yscale != nullptr) || (Kept != nullptr) != (Kscale != nullptr) ||
+        (R != nullptr) != (S != nullptr))
+        return LA_ERR_NULL;
+    const size_t e = la::size_of(dt), n = rows * C, pb = la::powers_bytes(rows, C);
+    for (const void *p : {X, R, (const void *)S, yt == dt ? (const void *)Y : nullptr})
+        if (!la::aligned_to(p, e)) return LA_ERR_ALIGN;
+    if ((W && !la::aligned_to(W, la::size_of(wt))) || !la::aligned_to(rstd, 4)) return LA_ERR_ALIGN;
+    const la::Range ins[] = {{X, n * e}, {R, S == R ? 0 : n * e}, {W, W ? C * la::size_of(wt) : 0}};
+    const la::Range outs[] = {{Y, n * la::size_of(yt)}, {Yscale, pb}, {S, n * e}, {Kept, n}, {Kscale, pb}, {rstd, rows * 4}};
+    if (la::any_alias(ins, 3, outs, 6)) return LA_ERR_ALIAS;
+    if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
+    const la::Norm a{X, R, W, Y, S, (uint8_t *)Yscale, (uint8_t *)Kept, (uint8_t *)Kscale, rstd, rows, C, eps, yt, kt};
+    const size_t groups = la::row_groups(rows, C);
+    const dim3 grid((unsigned)(groups < 65536 ? groups : 65536));
+    la::by_types(dt, wt, [&](auto *t, auto *w) {
+        la::by_width(C, [&](auto shape) {
+            typedef decltype(shape) Sh;
+            la::k_norm<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(w)>, Sh::l, Sh::k>
+                <<<grid, dim3(la::Share<Sh::l>::NT), 0, (hipStream_t)hip_stream>>>(a);
+        });
+    });
+    return la::done();
+}
+
+la_status la_rmsnorm_backward(const void *S, const void *Sscale, const void *W, const float *rstd, const void *dY,
+                              const void *dS, void *dX, float *dW, size_t rows, int C, la_dtype dt, la_dtype wt,
+                              la_dtype st, void *workspace, size_t workspace_bytes, void *hip_stream)
+{
+    const la_status s = la::check_rows(rows, C, la::kMostColumns);
+    if (s != LA_OK) return s;
+    if (!la::real_type(dt) || (W && wt != LA_F32 && wt != dt)) return LA_ERR_UNSUPPORTED;
+    if (st != dt && !la::eight_bits(st)) return LA_ERR_UNSUPPORTED;
+    if (!S || !rstd || !dY || !dX || (st != dt) != (Sscale != nullptr) || (dW && !W)) return LA_ERR_NULL;
+    const size_t e = la::size_of(dt), n = rows * C, need = dW ? la_rmsnorm_workspace_bytes(rows, C) : 0;
+    for (const void *p : {st == dt ? S : nullptr, dY, dS, (const void *)dX})
+        if (!la::aligned_to(p, e)) return LA_ERR_ALIGN;
+    if ((W && !la::aligned_to(W, la::size_of(wt))) || !la::aligned_to(rstd, 4) || !la::aligned_to(dW, 4))
+        return LA_ERR_ALIGN;
+    if (need && (!workspace || workspace_bytes < need || !la::aligned_to(workspace, 256))) return LA_ERR_WORKSPACE;
+    const la::Range ins[] = {{S, n * la::size_of(st)}, {Sscale, la::powers_bytes(rows, C)}, {W, W ? C * la::size_of(wt) : 0},
+                             {rstd, rows * 4}, {dY, n * e}, {dS, n * e}};
+    const la::Range outs[] = {{dX, n * e}, {dW, (size_t)C * 4}, {workspace, need}};
+    if (la::any_alias(ins, 6, outs, 3)) return LA_ERR_ALIAS;
+    if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
+    const la::NormBack a{S, W, dY, dS, (const uint8_t *)Sscale, rstd, dX, dW ? (float *)workspace : nullptr, rows, C, st};
+    const int blocks = la::back_blocks(la::row_groups(rows, C));
+    const hipStream_t stream = (hipStream_t)hip_stream;
+    la::by_types(dt, wt, [&](auto *t, auto *w) {
+        la::by_width(C, [&](auto shape) {
+            typedef decltype(shape) Sh;
+            la::k_norm_back<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(w)>, Sh::l, Sh::k>
+                <<<dim3(blocks), dim3(la::Share<Sh::l>::NT), 0, stream>>>(a);
+        });
+    });
+    if (dW) la::k_norm_join<<<dim3((C + 63) / 64), dim3(1024), 0, stream>>>((const float *)workspace, dW, blocks, C);
+    return la::done();
+}
+
+}  // extern "C"
