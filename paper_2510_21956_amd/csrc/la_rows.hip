@@ -71,11 +71,8 @@ __global__ void __launch_bounds__(Share<L>::NT) k_norm(Norm a)
             if (a.R) {
                 const Eight r = load8((const T *)a.R + at + c, valid);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) {  // as it is stored: what the backward pass will read
-                    T s[1];
-                    store_elem(s, 0, t[k].x[j] + r.x[j]);
-                    t[k].x[j] = load_elem(s, 0);
-                }
+                for (int j = 0; j < 8; ++j) t[k].x[j] += r.x[j];
+                t[k] = widen<T>(narrow<T>(t[k]));  // as it is stored: what the backward pass will read
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) ss[0] += t[k].x[j] * t[k].x[j];
@@ -86,7 +83,7 @@ __global__ void __launch_bounds__(Share<L>::NT) k_norm(Norm a)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = (k * L + lane) * 8, valid = here ? C - c : 0;
-            if (a.S) store8((T *)a.S + at + c, t[k], valid);
+            if (a.S) store8<true>((T *)a.S + at + c, t[k], valid);
             if (a.K) pack8(t[k], a.K + at, a.Kp + (here ? row : 0) * G, c, valid, a.kt == LA_I8);
             Eight y = t[k];
             if (a.W) {
@@ -98,7 +95,7 @@ __global__ void __launch_bounds__(Share<L>::NT) k_norm(Norm a)
                 for (int j = 0; j < 8; ++j) y.x[j] *= rstd;
             }
             if (a.Yp) pack8(y, (uint8_t *)a.Y + at, a.Yp + (here ? row : 0) * G, c, valid, a.yt == LA_I8);
-            else store8((T *)a.Y + at + c, y, valid);
+            else store8<true>((T *)a.Y + at + c, y, valid);
         }
     }
 }
@@ -131,23 +128,44 @@ __global__ void __launch_bounds__(Share<L>::NT) k_norm_back(NormBack a)
             dw[k].x[j] = 0.f;
         }
     }
-    for (size_t base = (size_t)blockIdx.x * Share<L>::ROWS; base < a.rows; base += step) {
-        const size_t row = base + threadIdx.x / L;
+    // a row's tensors, requested while the row before it is worked on where there are registers for it
+    constexpr bool AHEAD = K == 1;
+    Stored<T> ns[K], nd[K], ng[K];
+    uint2 nc[K];
+    int ne[K];
+    float nr = 0.f;
+    const auto request = [&](size_t row) {
         const bool here = row < a.rows;
         const size_t at = (here ? row : 0) * C;
-        const float rstd = here ? a.rstd[row] : 0.f;
-        Eight n[K], d[K];
-        float m[1] = {0.f};
+        nr = here ? a.rstd[row] : 0.f;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = (k * L + lane) * 8, valid = here ? C - c : 0;
             if (a.Sp) {
-                const uint2 codes = load_codes((const uint8_t *)a.S + at + c, valid);
-                const int e = valid > 0 ? a.Sp[row * G + c / kGroup] : 127;
-                n[k] = values_of(codes, e, a.st == LA_I8);
-            } else n[k] = load8((const T *)a.S + at + c, valid);
-            d[k] = load8((const T *)a.dY + at + c, valid);
+                nc[k] = load_codes((const uint8_t *)a.S + at + c, valid);
+                ne[k] = valid > 0 ? a.Sp[row * G + c / kGroup] : 127;
+            } else ns[k] = request8((const T *)a.S + at + c, valid);
+            nd[k] = request8((const T *)a.dY + at + c, valid);
+            if (a.dS) ng[k] = request8((const T *)a.dS + at + c, valid);
         }
+    };
+    if (AHEAD) request((size_t)blockIdx.x * Share<L>::ROWS + threadIdx.x / L);
+    for (size_t base = (size_t)blockIdx.x * Share<L>::ROWS; base < a.rows; base += step) {
+        const size_t row = base + threadIdx.x / L;
+        const bool here = row < a.rows;
+        const size_t at = (here ? row : 0) * C;
+        if (!AHEAD) request(row);
+        const float rstd = nr;
+        Eight n[K], d[K];
+        Stored<T> g[K];
+        float m[1] = {0.f};
+#pragma unroll
+        for (int k = 0; k < K; ++k) {
+            n[k] = a.Sp ? values_of(nc[k], ne[k], a.st == LA_I8) : widen<T>(ns[k]);
+            d[k] = widen<T>(nd[k]);
+            g[k] = ng[k];
+        }
+        if (AHEAD) request(row + step);
 #pragma unroll
         for (int k = 0; k < K; ++k)
 #pragma unroll
@@ -162,15 +180,14 @@ __global__ void __launch_bounds__(Share<L>::NT) k_norm_back(NormBack a)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = (k * L + lane) * 8, valid = here ? C - c : 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) d[k].x[j] = rstd * (d[k].x[j] - n[k].x[j] * mean);
             if (a.dS) {
-                const Eight s = load8((const T *)a.dS + at + c, valid);
+                const Eight s = widen<T>(g[k]);
 #pragma unroll
-                for (int j = 0; j < 8; ++j) d[k].x[j] = rstd * (d[k].x[j] - n[k].x[j] * mean) + s.x[j];
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) d[k].x[j] = rstd * (d[k].x[j] - n[k].x[j] * mean);
+                for (int j = 0; j < 8; ++j) d[k].x[j] += s.x[j];
             }
-            store8((T *)a.dX + at + c, d[k], valid);
+            store8<false>((T *)a.dX + at + c, d[k], valid);
         }
     }
     if (!a.parts) return;
@@ -192,7 +209,7 @@ __global__ void __launch_bounds__(Share<L>::NT) k_norm_back(NormBack a)
 #pragma unroll
         for (int k = 0; k < K; ++k) {
             const int c = (k * L + lane) * 8;
-            store8(out + c, dw[k], C - c);
+            store8<false>(out + c, dw[k], C - c);
         }
     }
 }
@@ -234,40 +251,65 @@ __global__ void __launch_bounds__(256) k_rows8(const T *X, T *Xout, const uint8_
             pack8(x, codes_out + row * C, powers_out + row * G, c, valid, ints);
         } else if (valid > 0) {
             const Eight x = values_of(load_codes(codes + row * C + c, valid), powers[row * G + c / kGroup], ints);
-            store8(Xout + row * C + c, x, valid);
+            store8<true>(Xout + row * C + c, x, valid);
         }
     }
 }
 
 constexpr int kMostColumns = 16384;  // of the norm, whose rows stay in registers
 
-// Workgroups of the backward pass: two a compute unit at most, so that the shares of dw are few.
-int back_blocks(size_t groups) { return (int)(groups < 512 ? groups : 512); }
-int row_lanes(int C) { return C <= 64 ? 8 : C <= 128 ? 16 : C <= 256 ? 32 : C <= 2048 ? 64 : C <= 8192 ? 256 : 1024; }
-size_t row_groups(size_t rows, int C)
-{
-    const int L = row_lanes(C), per = L > 256 ? 1 : 256 / L;
-    return (rows + per - 1) / per;
-}
-
-// Calls f with the shape (L, K) that holds a row of C elements.
+// Lanes that share a row of C elements, and steps.  Forward: two steps a lane, which leaves few lanes waiting
+// for a row's sum; backward: one, whose registers hold the next row as well.
 template <int L, int K>
 struct Shape {
     static constexpr int l = L, k = K;
 };
 template <typename F>
-void by_width(int C, F f)
+void by_width_short(int C, F f)
 {
     if (C <= 64) f(Shape<8, 1>());
     else if (C <= 128) f(Shape<16, 1>());
     else if (C <= 256) f(Shape<32, 1>());
-    else if (C <= 512) f(Shape<64, 1>());
+    else f(Shape<64, 1>());
+}
+template <typename F>
+void by_width(int C, F f)
+{
+    if (C <= 512) by_width_short(C, f);
     else if (C <= 1024) f(Shape<64, 2>());
-    else if (C <= 2048) f(Shape<64, 4>());
+    else if (C <= 2048) f(Shape<128, 2>());
     else if (C <= 4096) f(Shape<256, 2>());
-    else if (C <= 8192) f(Shape<256, 4>());
+    else if (C <= 8192) f(Shape<512, 2>());
     else f(Shape<1024, 2>());
 }
+template <typename F>
+void by_width_back(int C, F f)
+{
+    if (C <= 512) by_width_short(C, f);
+    else if (C <= 1024) f(Shape<128, 1>());
+    else if (C <= 2048) f(Shape<256, 1>());
+    else if (C <= 4096) f(Shape<512, 1>());
+    else if (C <= 8192) f(Shape<1024, 1>());
+    else f(Shape<1024, 2>());
+}
+// Workgroups that take all rows in one go.
+size_t row_groups(size_t rows, int L)
+{
+    const int per = L > 256 ? 1 : 256 / L;
+    return (rows + per - 1) / per;
+}
+// Workgroups of the backward pass: sixteen waves a compute unit, and few shares of dw.
+int back_blocks(size_t rows, int C)
+{
+    int n = 0;
+    by_width_back(C, [&](auto shape) {
+        typedef decltype(shape) Sh;
+        const size_t g = row_groups(rows, Sh::l), most = 4096 * 64 / Share<Sh::l>::NT;
+        n = (int)(g < most ? g : most);
+    });
+    return n;
+}
+
 template <typename F>
 void by_types(la_dtype dt, la_dtype wt, F f)
 {
@@ -338,7 +380,7 @@ la_status la_unpack_rows(const void *codes, const void *scales, void *X, size_t 
 size_t la_rmsnorm_workspace_bytes(size_t rows, int C)
 {
     if (la::check_rows(rows, C, la::kMostColumns) != LA_OK) return 0;
-    return la::round_up((size_t)la::back_blocks(la::row_groups(rows, C)) * C * 4, 256);
+    return la::round_up((size_t)la::back_blocks(rows, C) * C * 4, 256);
 }
 
 la_status la_rmsnorm_forward(const void *X, const void *R, const void *W, void *Y, void *Yscale, void *S, void *Kept,
@@ -361,11 +403,11 @@ la_status la_rmsnorm_forward(const void *X, const void *R, const void *W, void *
     if (la::any_alias(ins, 3, outs, 6)) return LA_ERR_ALIAS;
     if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
     const la::Norm a{X, R, W, Y, S, (uint8_t *)Yscale, (uint8_t *)Kept, (uint8_t *)Kscale, rstd, rows, C, eps, yt, kt};
-    const size_t groups = la::row_groups(rows, C);
-    const dim3 grid((unsigned)(groups < 65536 ? groups : 65536));
     la::by_types(dt, wt, [&](auto *t, auto *w) {
         la::by_width(C, [&](auto shape) {
             typedef decltype(shape) Sh;
+            const size_t groups = la::row_groups(rows, Sh::l);
+            const dim3 grid((unsigned)(groups < 65536 ? groups : 65536));
             la::k_norm<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(w)>, Sh::l, Sh::k>
                 <<<grid, dim3(la::Share<Sh::l>::NT), 0, (hipStream_t)hip_stream>>>(a);
         });
@@ -394,10 +436,10 @@ la_status la_rmsnorm_backward(const void *S, const void *Sscale, const void *W, 
     if (la::any_alias(ins, 6, outs, 3)) return LA_ERR_ALIAS;
     if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
     const la::NormBack a{S, W, dY, dS, (const uint8_t *)Sscale, rstd, dX, dW ? (float *)workspace : nullptr, rows, C, st};
-    const int blocks = la::back_blocks(la::row_groups(rows, C));
+    const int blocks = la::back_blocks(rows, C);
     const hipStream_t stream = (hipStream_t)hip_stream;
     la::by_types(dt, wt, [&](auto *t, auto *w) {
-        la::by_width(C, [&](auto shape) {
+        la::by_width_back(C, [&](auto shape) {
             typedef decltype(shape) Sh;
             la::k_norm_back<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(w)>, Sh::l, Sh::k>
                 <<<dim3(blocks), dim3(la::Share<Sh::l>::NT), 0, stream>>>(a);
