@@ -462,6 +462,8 @@ LA_API la_status la_recurrence_step(const void *X, const void *Gate, void *Hs, f
  *
  *   la_pack_rows:   X [rows, C] of `dt` (LA_F32 / LA_BF16) -> codes [rows, C], scales
  *                   [rows, ceil(C / 32)] bytes
+ *   la_pack_tensors: the same for `count` tensors of one shape (1 to 4), whose addresses are read
+ *                   before the call returns.
  *   la_unpack_rows: the way back.
  * One byte and 1/32 an element instead of two or four: what a backward pass keeps of a forward pass
  * where memory is short (la_rmsnorm_backward reads the codes themselves).
@@ -469,6 +471,9 @@ LA_API la_status la_recurrence_step(const void *X, const void *Gate, void *Hs, f
  */
 LA_API la_status la_pack_rows(const void *X, void *codes, void *scales, size_t rows, int C,
                      la_dtype dt, la_dtype code, void *hip_stream);
+
+LA_API la_status la_pack_tensors(int count, const void *const *X, void *const *codes, void *const *scales,
+                     size_t rows, int C, la_dtype dt, la_dtype code, void *hip_stream);
 
 LA_API la_status la_unpack_rows(const void *codes, const void *scales, void *X, size_t rows, int C,
                      la_dtype code, la_dtype dt, void *hip_stream);

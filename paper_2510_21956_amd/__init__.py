@@ -10,7 +10,7 @@ from .binding import (EXPORTS, LA_BF16, LA_F32, LA_MAX_TRACE, LaError, la_backwa
                       la_backward_saved, la_backward_traced, la_forward, la_forward_save,
                       la_forward_traced, la_saved_state_bytes, la_status_string, la_trace,
                       la_version, la_workspace_bytes, library_path, load_library)
-from .binding import (LA_E4M3, LA_GATE_SIGMOID, LA_GATE_VALUE, LA_GROUP, LA_I8, la_pack_rows, la_recurrence_backward,
+from .binding import (LA_E4M3, LA_GATE_SIGMOID, LA_GATE_VALUE, LA_GROUP, LA_I8, la_pack_rows, la_pack_tensors, la_recurrence_backward,
                       la_recurrence_forward, la_recurrence_step, la_recurrence_workspace_bytes, la_rmsnorm_backward,
                       la_rmsnorm_forward, la_rmsnorm_workspace_bytes, la_unpack_rows)
 
@@ -23,5 +23,5 @@ __all__ = ["LinearAttentionFunction", "linear_attention", "LA_F32", "LA_BF16", "
            "la_status_string", "la_version", "library_path", "load_library",
            "gated_recurrence", "rms_norm", "rms_norm_quantised", "pack_rows", "unpack_rows", "LA_E4M3", "LA_I8",
            "LA_GROUP", "LA_GATE_VALUE", "LA_GATE_SIGMOID", "la_recurrence_workspace_bytes", "la_recurrence_forward",
-           "la_recurrence_backward", "la_recurrence_step", "la_pack_rows", "la_unpack_rows",
+           "la_recurrence_backward", "la_recurrence_step", "la_pack_rows", "la_pack_tensors", "la_unpack_rows",
            "la_rmsnorm_workspace_bytes", "la_rmsnorm_forward", "la_rmsnorm_backward"]

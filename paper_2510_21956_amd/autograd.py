@@ -74,25 +74,29 @@ class CheckpointedAttentionFunction(torch.autograd.Function):
         O = torch.empty_like(Q)
         ws = _bytes(_b.la_workspace_bytes(B, H, N, D, dt, causal, 0), Q.device)
         (_b.la_forward_qknorm if normalize_qk else _b.la_forward)(Q, K, V, O, None, a, b, causal, ws)
-        ctx.save_for_backward(*(t for x in (Q, K, V) for t in pack_rows(x, code)))
-        ctx.la_args = (float(a), float(b), bool(causal), bool(normalize_qk))
-        ctx.la_code, ctx.la_dtype = code, Q.dtype
+        codes, scales = _eight_bits(Q, code, 3)
+        _b.la_pack_tensors([Q, K, V], list(codes), list(scales), code)
+        ctx.save_for_backward(codes, scales)
+        ctx.la_args = (float(a), float(b), bool(causal), bool(normalize_qk), code, Q.dtype == torch.float32)
         return O
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dO):
-        kept, (a, b, causal, normalize_qk) = ctx.saved_tensors, ctx.la_args
-        Q, K, V = (unpack_rows(kept[i], kept[i + 1], ctx.la_code, ctx.la_dtype) for i in (0, 2, 4))
-        B, H, N, D = Q.shape
-        dt = _code(Q)
-        O, G = torch.empty_like(Q), torch.empty((B, H, N), dtype=torch.float32, device=Q.device)
-        ws = _bytes(_b.la_workspace_bytes(B, H, N, D, dt, causal, 0), Q.device)
-        ns = _b.la_saved_state_bytes(B, H, N, D, dt, causal)
-        saved = _bytes(ns, Q.device) if ns else None
-        fwd = _b.la_forward_qknorm_save if normalize_qk else _b.la_forward_save
-        fwd(Q, K, V, O, G, a, b, causal, ws, saved)
-        return (*python_backward(Q, K, V, O, G, dO, saved, a, b, causal, normalize_qk), None, None, None, None, None)
+        return (*checkpointed_backward(*ctx.saved_tensors, dO.contiguous(), *ctx.la_args), None, None, None, None, None)
+
+
+def checkpointed_backward(codes, scales, dO, a, b, causal, normalize_qk, code, single):
+    Q, K, V = unpack_rows(codes, scales, code, torch.float32 if single else torch.bfloat16)
+    B, H, N, D = Q.shape
+    dt = _code(Q)
+    O, G = torch.empty_like(Q), torch.empty((B, H, N), dtype=torch.float32, device=Q.device)
+    ws = _bytes(_b.la_workspace_bytes(B, H, N, D, dt, causal, 0), Q.device)
+    ns = _b.la_saved_state_bytes(B, H, N, D, dt, causal)
+    saved = _bytes(ns, Q.device) if ns else None
+    fwd = _b.la_forward_qknorm_save if normalize_qk else _b.la_forward_save
+    fwd(Q, K, V, O, G, a, b, causal, ws, saved)
+    return python_backward(Q, K, V, O, G, dO, saved, a, b, bool(causal), bool(normalize_qk))
 
 
 def linear_attention(Q, K, V, a=1.0, b=0.5, causal=True, normalize_qk=False, checkpoint=None):
@@ -106,6 +110,9 @@ def linear_attention(Q, K, V, a=1.0, b=0.5, causal=True, normalize_qk=False, che
         code = _b.eight_bit_code(checkpoint)
         if Q.shape != K.shape or Q.shape != V.shape:
             raise ValueError("shape mismatch")
+        O = _b.in_native_code("checkpointed", "la_forward_save", Q, K, V, a, b, causal, normalize_qk, code)
+        if O is not None:
+            return O
         return CheckpointedAttentionFunction.apply(Q, K, V, a, b, causal, normalize_qk, code)
     O = _b.attention(Q, K, V, a, b, causal, normalize_qk)
     if O is not None:
@@ -132,11 +139,11 @@ def unpack_rows(codes, scales, code, dtype):
     return x
 
 
-def _eight_bits(x, code):
-    """Room for x's codes and powers."""
+def _eight_bits(x, code, *count):
+    """Room for x's codes and powers (for `count` tensors like x)."""
     kind = torch.float8_e4m3fn if code == _b.LA_E4M3 else torch.int8
-    groups = (*x.shape[:-1], -(-x.shape[-1] // _b.LA_GROUP))
-    return (torch.empty(x.shape, dtype=kind, device=x.device),
+    groups = (*count, *x.shape[:-1], -(-x.shape[-1] // _b.LA_GROUP))
+    return (torch.empty((*count, *x.shape), dtype=kind, device=x.device),
             torch.empty(groups, dtype=torch.float8_e8m0fnu, device=x.device))
 
 
@@ -162,14 +169,17 @@ class GatedRecurrenceFunction(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dh, dlast):
-        x, gates, h0, h, lengths = ctx.saved_tensors
+        x = ctx.saved_tensors[0]
         dh = torch.zeros_like(x) if dh is None else dh.contiguous()
         dlast = dlast if dlast is None else dlast.contiguous()
-        dx, dgates = torch.empty_like(x), torch.empty_like(x)
-        dh0 = torch.empty_like(h0) if ctx.needs_input_grad[2] else None
-        _b.la_recurrence_backward(x, gates, h0, h, dh, dlast, dx, dgates, dh0, lengths, ctx.la_gate,
-                                  _recurrence_room(x, 1))
-        return dx, dgates, dh0, None, None
+        return (*recurrence_backward(*ctx.saved_tensors, dh, dlast, ctx.la_gate, ctx.needs_input_grad[2]), None, None)
+
+
+def recurrence_backward(x, gates, h0, h, lengths, dh, dlast, gate, wants_h0):
+    dx, dgates = torch.empty_like(x), torch.empty_like(x)
+    dh0 = torch.empty_like(h0) if wants_h0 else None
+    _b.la_recurrence_backward(x, gates, h0, h, dh, dlast, dx, dgates, dh0, lengths, gate, _recurrence_room(x, 1))
+    return dx, dgates, dh0
 
 
 def _recurrence_room(x, is_backward):
@@ -189,6 +199,9 @@ def gated_recurrence(x, gates, h0=None, lengths=None, gate="sigmoid"):
     from which la_recurrence_step goes on."""
     if gate not in _GATES:
         raise ValueError("gates are %s, got %r" % (" and ".join(map(repr, _GATES)), gate))
+    out = _b.in_native_code("recurrence", "la_recurrence_forward", x, gates, h0, lengths, _GATES[gate])
+    if out is not None:
+        return out
     return GatedRecurrenceFunction.apply(x, gates, h0, lengths, _GATES[gate])
 
 
@@ -213,19 +226,22 @@ class RmsNormFunction(torch.autograd.Function):
     @staticmethod
     @once_differentiable
     def backward(ctx, dy, dtotal):
-        total, scales, weight, rstd = ctx.saved_tensors
         if dy is None:  # the sum alone was used
             return dtotal, dtotal if ctx.needs_input_grad[1] else None, None, None, None
-        dy = dy.contiguous()
         dtotal = dtotal if dtotal is None else dtotal.contiguous()
-        dx = torch.empty_like(dy)
-        dw = ws = None
-        if ctx.needs_input_grad[2]:
-            C = dy.shape[-1]
-            dw = torch.empty(C, dtype=torch.float32, device=dy.device)
-            ws = _bytes(_b.la_rmsnorm_workspace_bytes(dy.numel() // C, C), dy.device)
-        _b.la_rmsnorm_backward(total, scales, weight, rstd, dy, dtotal, dx, dw, ws, ctx.la_code)
-        return dx, dx if ctx.needs_input_grad[1] else None, dw if dw is None else dw.to(weight.dtype), None, None
+        return (*norm_backward(*ctx.saved_tensors, dy.contiguous(), dtotal, -1 if ctx.la_code is None else ctx.la_code,
+                               ctx.needs_input_grad[1], ctx.needs_input_grad[2]), None, None)
+
+
+def norm_backward(total, scales, weight, rstd, dy, dtotal, code, wants_residual, wants_weight):
+    dx = torch.empty_like(dy)
+    dw = ws = None
+    if wants_weight:
+        C = dy.shape[-1]
+        dw = torch.empty(C, dtype=torch.float32, device=dy.device)
+        ws = _bytes(_b.la_rmsnorm_workspace_bytes(dy.numel() // C, C), dy.device)
+    _b.la_rmsnorm_backward(total, scales, weight, rstd, dy, dtotal, dx, dw, ws, None if code < 0 else code)
+    return dx, dx if wants_residual else None, dw if dw is None else dw.to(weight.dtype)
 
 
 def rms_norm(x, weight=None, residual=None, eps=1e-6, checkpoint=None):
@@ -235,14 +251,19 @@ def rms_norm(x, weight=None, residual=None, eps=1e-6, checkpoint=None):
 
     ``checkpoint`` "e4m3" or "int8" keeps s in 8 bits for the backward pass, which then goes by those."""
     code = None if checkpoint is None else _b.eight_bit_code(checkpoint)
-    y, total = RmsNormFunction.apply(x, residual, weight, float(eps), code)
-    return y if residual is None else (y, total)
+    out = _b.in_native_code("norm", "la_rmsnorm_forward", x, weight, residual, eps, -1 if code is None else code)
+    if out is None:
+        out = RmsNormFunction.apply(x, residual, weight, float(eps), code)
+    return out[0] if residual is None else out
 
 
 def rms_norm_quantised(x, weight=None, residual=None, eps=1e-6, code="e4m3"):
     """rms_norm with y in 8 bits, for a matrix product on 8-bit operands: codes like x (float8_e4m3fn or
     int8) and scales [..., ceil(C / 32)] (float8_e8m0fnu), and s where there is a residual.  Not differentiable."""
     code = _b.eight_bit_code(code)
+    out = _b.in_native_code("norm_quantised", "la_rmsnorm_forward", x, weight, residual, eps, code)
+    if out is not None:
+        return out
     x = x.detach().contiguous()
     residual = residual if residual is None else residual.detach().contiguous()
     weight = weight if weight is None else weight.detach().contiguous()

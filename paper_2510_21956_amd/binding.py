@@ -34,7 +34,7 @@ EXPORTS = ("la_version", "la_status_string", "la_workspace_bytes", "la_forward",
            "la_decode_step", "la_decode_prefill", "la_backward_ab", "la_forward_qknorm",
            "la_backward_qknorm", "la_forward_qknorm_save", "la_backward_qknorm_saved",
            "la_recurrence_workspace_bytes", "la_recurrence_forward", "la_recurrence_backward",
-           "la_recurrence_step", "la_pack_rows", "la_unpack_rows", "la_rmsnorm_workspace_bytes",
+           "la_recurrence_step", "la_pack_rows", "la_pack_tensors", "la_unpack_rows", "la_rmsnorm_workspace_bytes",
            "la_rmsnorm_forward", "la_rmsnorm_backward")
 
 
@@ -117,6 +117,8 @@ def load_library():
     lib.la_recurrence_step.argtypes = [vp] * 4 + [i] * 5 + [vp]
     lib.la_pack_rows.restype = i
     lib.la_pack_rows.argtypes = [vp, vp, vp, sz, i, i, i, vp]
+    lib.la_pack_tensors.restype = i
+    lib.la_pack_tensors.argtypes = [i, ctypes.POINTER(vp), ctypes.POINTER(vp), ctypes.POINTER(vp), sz, i, i, i, vp]
     lib.la_unpack_rows.restype = i
     lib.la_unpack_rows.argtypes = [vp, vp, vp, sz, i, i, i, vp]
     lib.la_rmsnorm_workspace_bytes.restype = sz
@@ -159,6 +161,13 @@ def _open_native(lib):
         lib.la_backward_traced, lib.la_backward_qknorm, lib.la_backward_saved,
         lib.la_backward_qknorm_saved, lib.la_decode_step, lib.la_decode_prefill, lib.la_workspace_bytes,
         lib.la_saved_state_bytes)))
+    module.init_layer(autograd.recurrence_backward, autograd.norm_backward, autograd.checkpointed_backward, *(
+        ctypes.cast(f, ctypes.c_void_p).value for f in (
+            lib.la_recurrence_workspace_bytes, lib.la_recurrence_forward, lib.la_recurrence_backward, lib.la_recurrence_step,
+            lib.la_pack_tensors, lib.la_unpack_rows, lib.la_rmsnorm_workspace_bytes, lib.la_rmsnorm_forward,
+            lib.la_rmsnorm_backward, lib.la_forward_traced, lib.la_forward_qknorm, lib.la_forward_save,
+            lib.la_forward_qknorm_save, lib.la_backward_saved, lib.la_backward_qknorm_saved, lib.la_workspace_bytes,
+            lib.la_saved_state_bytes)))
     return module
 
 
@@ -587,6 +596,12 @@ def la_recurrence_backward(x, gates, h0, h, dh, dlast, dx, dgates, dh0, lengths,
 
 def la_recurrence_step(x, gates, h, state, gate, stream=None):
     """la_recurrence_step of include/la.h: x, gates, h [..., T, C]; state [..., C] float32, updated in place."""
+    if _native is not None:
+        rc = _native.recurrence_step(x, gates, h, state, gate, stream)
+        if rc == 0:
+            return
+        if rc is not None:
+            raise LaError(rc, "la_recurrence_step")
     _needed(x=x, gates=gates, h=h, state=state)
     _check_tensors(x, gates, h, state)
     _like(x, gates=gates, h=h)
@@ -632,6 +647,21 @@ def la_pack_rows(x, codes, scales, code, stream=None):
     _eight(codes, scales, x, code, "packed")
     rows, C = _rows(x)
     _call("la_pack_rows", x, stream, _ptr(x), _ptr(codes), _ptr(scales), rows, C, _real_code(x), int(code))
+
+
+def la_pack_tensors(xs, codes, scales, code, stream=None):
+    """la_pack_tensors of include/la.h: lists of one to four tensors of one shape, as for la_pack_rows."""
+    if not len(xs) == len(codes) == len(scales) or not xs:
+        raise ValueError("as many codes and scales as tensors are needed")
+    _needed(x=xs[0])
+    _check_tensors(xs[0], *xs, *codes, *scales)
+    for x, c, s in zip(xs, codes, scales):
+        _needed(x=x)
+        _like(xs[0], x=x)
+        _eight(c, s, x, code, "packed")
+    rows, C = _rows(xs[0])
+    lists = [(ctypes.c_void_p * len(ts))(*map(_ptr, ts)) for ts in (xs, codes, scales)]
+    _call("la_pack_tensors", xs[0], stream, len(xs), *lists, rows, C, _real_code(xs[0]), int(code))
 
 
 def la_unpack_rows(codes, scales, x, code, stream=None):
@@ -711,3 +741,16 @@ def la_rmsnorm_backward(total, scales, weight, rstd, dy, dtotal, dx, dweight, wo
     rows, C = _rows(dy)
     _call("la_rmsnorm_backward", dy, stream, _ptr(total), _ptr(scales), _ptr(weight), _ptr(rstd), _ptr(dy), _ptr(dtotal),
           _ptr(dx), _ptr(dweight), rows, C, dt, wt, dt if code is None else int(code), *_room(workspace))
+
+
+def in_native_code(name, where, *args):
+    """The result of one of the native functions of csrc/la_bind_layer.cpp; None where there is none, or what it is
+    given is left to the Python code."""
+    if _native is None:
+        load_library()
+        if _native is None:
+            return None
+    out = getattr(_native, name)(*args)
+    if type(out) is int:
+        raise LaError(out, where)
+    return out

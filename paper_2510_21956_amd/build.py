@@ -56,7 +56,7 @@ def _compile_marshal(verbose, out):
            "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch._C._GLIBCXX_USE_CXX11_ABI, "-D__HIP_PLATFORM_AMD__", "-DUSE_ROCM",
            '-DLA_BUILT_FOR="torch %s, Python %d.%d"' % (torch.__version__, *sys.version_info[:2]), "-I", INCLUDE]
     cmd += ["-isystem%s" % p for p in include_paths() + [os.path.join(ROCM, "include"), sysconfig.get_paths()["include"]]]
-    cmd += [os.path.join(CSRC, "la_bind.cpp")]
+    cmd += sorted(glob.glob(os.path.join(CSRC, "la_bind*.cpp")))
     cmd += ["-L%s" % p for p in library_paths()] + ["-ltorch_python", "-ltorch_cpu", "-lc10_hip", "-lc10", "-o", out]
     if verbose:
         print(" ".join(cmd))

@@ -6,23 +6,12 @@
 // Refuses nothing itself: what does not pass the checks (a tensor without storage or a functorch wrapper, whose
 // C++ exception ends up here, included) goes back to the Python functions, which refuse or take it.  The library
 // is called without the interpreter lock, as ctypes does.
-#include <ATen/FuncTorchTLS.h>
-#include <ATen/PythonTorchFunctionTLS.h>
-#include <ATen/ops/empty.h>
-#include <ATen/ops/empty_like.h>
-#include <c10/core/impl/TorchDispatchModeTLS.h>
-#include <c10/hip/HIPStream.h>
-#include <torch/csrc/Exceptions.h>
-#include <torch/csrc/autograd/custom_function.h>
-#include <torch/csrc/autograd/python_cpp_function.h>
-#include <torch/csrc/autograd/python_variable.h>
-#include <torch/csrc/jit/frontend/tracer.h>
+#include "la_bind.h"
 
-#include "la.h"
+PyObject *raw_stream = nullptr;
 
 namespace {
 
-PyObject *raw_stream = nullptr;       // device index -> stream handle of its current stream
 PyObject *python_backward = nullptr;  // the wrapper's backward pass in Python
 
 // Entry points of libla.so, as addresses (binding.py has loaded the library).
@@ -34,103 +23,6 @@ decltype(&la_decode_step) dec_step;
 decltype(&la_decode_prefill) dec_prefill;
 decltype(&la_workspace_bytes) workspace_bytes;
 decltype(&la_saved_state_bytes) saved_state_bytes;
-
-struct Decline {};  // the Python function takes over; a Python exception may be set
-void require(bool ok)
-{
-    if (!ok) throw Decline();
-}
-
-bool is_none(PyObject *o) { return o == Py_None; }
-// Tensors and parameters; a subclass may answer is_contiguous, data_ptr and the rest in its own way, which
-// the Python functions ask it for.
-bool plain(PyObject *o) { return THPVariable_CheckExact(o); }
-bool plain_or_none(PyObject *o) { return is_none(o) || plain(o); }
-const at::Tensor &tensor(PyObject *o) { return THPVariable_Unpack(o); }
-void *address(PyObject *o) { return is_none(o) ? nullptr : tensor(o).data_ptr(); }
-size_t bytes(const at::Tensor &t) { return (size_t)t.numel() * t.element_size(); }
-
-// Packed device tensors, all on one device (None is left out).
-void check_packed(std::initializer_list<PyObject *> ts)
-{
-    const at::Tensor &ref = tensor(*ts.begin());
-    for (PyObject *o : ts) {
-        if (is_none(o)) continue;
-        const at::Tensor &t = tensor(o);
-        require(t.is_cuda() && t.is_contiguous() && t.get_device() == ref.get_device());
-    }
-}
-void check_like(const at::Tensor &ref, std::initializer_list<PyObject *> ts)
-{
-    for (PyObject *o : ts)
-        require(is_none(o) || (tensor(o).sizes() == ref.sizes() && tensor(o).scalar_type() == ref.scalar_type()));
-}
-void check_rows(const at::Tensor &ref, PyObject *g)
-{
-    if (is_none(g)) return;
-    const at::Tensor &t = tensor(g);
-    require(t.sizes() == ref.sizes().slice(0, 3) && t.scalar_type() == at::kFloat);
-}
-la_dtype dtype_code(const at::Tensor &t)
-{
-    require(t.scalar_type() == at::kFloat || t.scalar_type() == at::kBFloat16);
-    return t.scalar_type() == at::kFloat ? LA_F32 : LA_BF16;
-}
-double real(PyObject *o)
-{
-    if (PyFloat_CheckExact(o)) return PyFloat_AS_DOUBLE(o);
-    PyObject *f = PyNumber_Float(o);  // what float(o) gives
-    require(f);
-    const double x = PyFloat_AS_DOUBLE(f);
-    Py_DECREF(f);
-    return x;
-}
-float number(PyObject *o) { return (float)real(o); }
-int truth(PyObject *o)
-{
-    const int x = PyObject_IsTrue(o);
-    require(x >= 0);
-    return x;
-}
-void *stream_of(PyObject *stream, const at::Tensor &ref)
-{
-    PyObject *h = is_none(stream) ? PyObject_CallFunction(raw_stream, "i", (int)ref.get_device())
-                                  : PyObject_GetAttrString(stream, "cuda_stream");
-    require(h);
-    void *p = PyLong_AsVoidPtr(h);
-    Py_DECREF(h);
-    require(p || !PyErr_Occurred());
-    return p;
-}
-
-// Runs body, which returns the library's status, on n arguments.  None: the Python function takes over.
-template <typename Body>
-PyObject *guarded(Py_ssize_t given, Py_ssize_t n, Body body)
-{
-    if (given != n) return PyErr_Format(PyExc_TypeError, "%zd arguments expected", n);
-    try {
-        return body();
-    } catch (const Decline &) {
-    } catch (const std::exception &) {
-    }
-    if (PyErr_Occurred() && !PyErr_ExceptionMatches(PyExc_Exception)) return nullptr;  // an interrupt
-    PyErr_Clear();
-    Py_RETURN_NONE;
-}
-template <typename Call>
-PyObject *status(Call call)
-{
-    la_status s;
-    Py_BEGIN_ALLOW_THREADS s = call();
-    Py_END_ALLOW_THREADS return PyLong_FromLong(s);
-}
-bool ours(PyObject *const *a, int first, int last)
-{
-    if (!plain(a[first])) return false;
-    for (int i = first + 1; i <= last; ++i)
-        if (!plain_or_none(a[i])) return false;
-    return true;
-}
 
 // kind (0 plain, 1 save, 2 qknorm, 3 qknorm_save), Q, K, V, O, G, a, b, causal, workspace, saved, stream
 PyObject *forward(PyObject *, PyObject *const *x, Py_ssize_t n)
@@ -255,15 +147,6 @@ PyObject *decode_prefill(PyObject *, PyObject *const *x, Py_ssize_t n)
 // step, without the interpreter, whose lock the engine's thread otherwise waits for in the backward pass.  Forward
 // and backward pass of a toy layer (1 slice of 256 rows, D = 16): 117 -> 83 us, nearly all of it host.
 
-at::Tensor buffer(size_t n, const at::Tensor &ref)
-{
-    return at::empty({(int64_t)(n < 256 ? 256 : n)}, ref.options().dtype(at::kByte));
-}
-void *current_stream(const at::Tensor &ref) { return c10::hip::getCurrentHIPStream(ref.get_device()).stream(); }
-
-struct Status {  // what the library answered
-    int rc;
-};
 struct Attention : torch::autograd::Function<Attention> {
     static at::Tensor forward(torch::autograd::AutogradContext *ctx, const at::Tensor &Q0, const at::Tensor &K0,
                               const at::Tensor &V0, double a, double b, bool causal, bool norm)
@@ -412,14 +295,7 @@ PyObject *attention(PyObject *, PyObject *const *x, Py_ssize_t n)
         require(Q.dim() == 4 && Q.is_cuda());
         dtype_code(Q);
         check_like(Q, {x[1], x[2]});
-        for (int i = 0; i < 3; ++i)
-            require(tensor(x[i]).is_cuda() && tensor(x[i]).get_device() == Q.get_device() &&
-                    !tensor(x[i])._fw_grad(0).defined());
-        for (int i = 0; i < 3; ++i) tensor(x[i]).const_data_ptr();  // throws where there is no storage
-        require(!at::impl::torch_function_mode_enabled() && !c10::impl::TorchDispatchModeTLS::any_modes_set() &&
-                !torch::jit::tracer::isTracing());
-        if (const auto &transforms = at::functorch::functorchTLSAccessor())
-            transforms->checkSupportsCppAutogradFunction();  // throws inside of vmap, grad and the like
+        check_inputs(Q, {x[0], x[1], x[2]});
         // a tensor among the coefficients and switches is an input of the Python node: its grad makes O require one
         for (int i = 3; i < 7; ++i)
             require(PyFloat_CheckExact(x[i]) || PyLong_Check(x[i]) || !THPVariable_Check(x[i]));
@@ -475,6 +351,7 @@ PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)())init, METH_FASTCALL, 
                          {"attention", (PyCFunction)(void (*)())attention, METH_FASTCALL, nullptr},
                          {"decode_step", (PyCFunction)(void (*)())decode_step, METH_FASTCALL, nullptr},
                          {"decode_prefill", (PyCFunction)(void (*)())decode_prefill, METH_FASTCALL, nullptr},
+                         {"init_layer", (PyCFunction)(void (*)())init_layer, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -483,6 +360,7 @@ PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, n
 PyMODINIT_FUNC PyInit__marshal()
 {
     PyObject *m = PyModule_Create(&module);
+    if (m && PyModule_AddFunctions(m, layer_methods) < 0) Py_CLEAR(m);
     if (m && PyModule_AddStringConstant(m, "built_for", LA_BUILT_FOR) < 0) Py_CLEAR(m);
     return m;
 }

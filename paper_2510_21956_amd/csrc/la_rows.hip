@@ -234,11 +234,19 @@ __global__ void __launch_bounds__(1024) k_norm_join(const float *parts, float *d
     }
 }
 
+// Tensors of one shape, blockIdx.y of them.
+constexpr int kMostTensors = 4;
+struct Batch {
+    const void *X[kMostTensors];
+    uint8_t *codes[kMostTensors], *powers[kMostTensors];
+};
+
 // Eight elements a lane; four lanes to a group, and as many to the last group of a row however short it is.
-template <typename T, bool PACK>
-__global__ void __launch_bounds__(256) k_rows8(const T *X, T *Xout, const uint8_t *codes, uint8_t *codes_out,
-                                               const uint8_t *powers, uint8_t *powers_out, size_t rows, int C, int ints)
+template <typename T>
+__global__ void __launch_bounds__(256) k_pack(Batch a, size_t rows, int C, int ints)
 {
+    const T *X = (const T *)a.X[blockIdx.y];
+    uint8_t *codes = a.codes[blockIdx.y], *powers = a.powers[blockIdx.y];
     const int G = (C + kGroup - 1) / kGroup, lanes = G * 4;
     const size_t total = rows * lanes, step = (size_t)gridDim.x * 256;
     for (size_t base = (size_t)blockIdx.x * 256; base < total; base += step) {
@@ -246,13 +254,19 @@ __global__ void __launch_bounds__(256) k_rows8(const T *X, T *Xout, const uint8_
         const bool here = i < total;
         const size_t row = here ? i / lanes : 0;
         const int c = here ? (int)(i - row * lanes) * 8 : 0, valid = here ? C - c : 0;
-        if constexpr (PACK) {
-            const Eight x = load8(X + row * C + c, valid);
-            pack8(x, codes_out + row * C, powers_out + row * G, c, valid, ints);
-        } else if (valid > 0) {
-            const Eight x = values_of(load_codes(codes + row * C + c, valid), powers[row * G + c / kGroup], ints);
-            store8<true>(Xout + row * C + c, x, valid);
-        }
+        pack8(load8(X + row * C + c, valid), codes + row * C, powers + row * G, c, valid, ints);
+    }
+}
+template <typename T>
+__global__ void __launch_bounds__(256) k_unpack(const uint8_t *codes, const uint8_t *powers, T *X, size_t rows, int C, int ints)
+{
+    const int G = (C + kGroup - 1) / kGroup, lanes = G * 4;
+    const size_t total = rows * lanes, step = (size_t)gridDim.x * 256;
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < total; i += step) {
+        const size_t row = i / lanes;
+        const int c = (int)(i - row * lanes) * 8, valid = C - c;
+        if (valid > 0)
+            store8<true>(X + row * C + c, values_of(load_codes(codes + row * C + c, valid), powers[row * G + c / kGroup], ints), valid);
     }
 }
 
@@ -327,19 +341,10 @@ la_status check_rows(size_t rows, int C, int most)
 size_t powers_bytes(size_t rows, int C) { return rows * ((C + kGroup - 1) / kGroup); }
 la_status done() { return hipGetLastError() == hipSuccess ? LA_OK : LA_ERR_LAUNCH; }
 
-template <bool PACK>
-la_status rows8(const void *X, void *Xo, const void *codes, void *codes_o, const void *powers, void *powers_o,
-                size_t rows, int C, la_dtype dt, la_dtype code, hipStream_t st)
+unsigned rows_blocks(size_t rows, int C)
 {
-    const size_t lanes = powers_bytes(rows, C) * 4, blocks = (lanes + 255) / 256;
-    const dim3 grid((unsigned)(blocks < 16384 ? blocks : 16384)), block(256);
-    if (dt == LA_F32)
-        k_rows8<float, PACK><<<grid, block, 0, st>>>((const float *)X, (float *)Xo, (const uint8_t *)codes, (uint8_t *)codes_o,
-                                                     (const uint8_t *)powers, (uint8_t *)powers_o, rows, C, code == LA_I8);
-    else
-        k_rows8<bf16_t, PACK><<<grid, block, 0, st>>>((const bf16_t *)X, (bf16_t *)Xo, (const uint8_t *)codes, (uint8_t *)codes_o,
-                                                      (const uint8_t *)powers, (uint8_t *)powers_o, rows, C, code == LA_I8);
-    return done();
+    const size_t blocks = (powers_bytes(rows, C) * 4 + 255) / 256;
+    return (unsigned)(blocks < 16384 ? blocks : 16384);
 }
 
 }  // namespace
@@ -347,19 +352,37 @@ la_status rows8(const void *X, void *Xo, const void *codes, void *codes_o, const
 
 extern "C" {
 
-la_status la_pack_rows(const void *X, void *codes, void *scales, size_t rows, int C, la_dtype dt, la_dtype code,
-                       void *hip_stream)
+la_status la_pack_tensors(int count, const void *const *X, void *const *codes, void *const *scales, size_t rows, int C,
+                          la_dtype dt, la_dtype code, void *hip_stream)
 {
     const la_status s = la::check_rows(rows, C, 2147483647 - 64);
     if (s != LA_OK) return s;
+    if (count < 1 || count > la::kMostTensors) return LA_ERR_SHAPE;
     if (!la::real_type(dt) || !la::eight_bits(code)) return LA_ERR_UNSUPPORTED;
     if (!X || !codes || !scales) return LA_ERR_NULL;
-    if (!la::aligned_to(X, la::size_of(dt))) return LA_ERR_ALIGN;
-    const la::Range ins[] = {{X, rows * C * la::size_of(dt)}};
-    const la::Range outs[] = {{codes, rows * C}, {scales, la::powers_bytes(rows, C)}};
-    if (la::any_alias(ins, 1, outs, 2)) return LA_ERR_ALIAS;
+    la::Batch a{};
+    la::Range ins[la::kMostTensors], outs[2 * la::kMostTensors];
+    for (int i = 0; i < count; ++i) {
+        if (!X[i] || !codes[i] || !scales[i]) return LA_ERR_NULL;
+        if (!la::aligned_to(X[i], la::size_of(dt))) return LA_ERR_ALIGN;
+        a.X[i] = X[i], a.codes[i] = (uint8_t *)codes[i], a.powers[i] = (uint8_t *)scales[i];
+        ins[i] = {X[i], rows * C * la::size_of(dt)};
+        outs[2 * i] = {codes[i], rows * C};
+        outs[2 * i + 1] = {scales[i], la::powers_bytes(rows, C)};
+    }
+    if (la::any_alias(ins, count, outs, 2 * count)) return LA_ERR_ALIAS;
     if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
-    return la::rows8<true>(X, nullptr, nullptr, codes, nullptr, scales, rows, C, dt, code, (hipStream_t)hip_stream);
+    const dim3 grid(la::rows_blocks(rows, C), count), block(256);
+    const hipStream_t st = (hipStream_t)hip_stream;
+    if (dt == LA_F32) la::k_pack<float><<<grid, block, 0, st>>>(a, rows, C, code == LA_I8);
+    else la::k_pack<la::bf16_t><<<grid, block, 0, st>>>(a, rows, C, code == LA_I8);
+    return la::done();
+}
+
+la_status la_pack_rows(const void *X, void *codes, void *scales, size_t rows, int C, la_dtype dt, la_dtype code,
+                       void *hip_stream)
+{
+    return la_pack_tensors(1, &X, &codes, &scales, rows, C, dt, code, hip_stream);
 }
 
 la_status la_unpack_rows(const void *codes, const void *scales, void *X, size_t rows, int C, la_dtype code,
@@ -374,7 +397,12 @@ la_status la_unpack_rows(const void *codes, const void *scales, void *X, size_t 
     const la::Range outs[] = {{X, rows * C * la::size_of(dt)}};
     if (la::any_alias(ins, 2, outs, 1)) return LA_ERR_ALIAS;
     if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
-    return la::rows8<false>(nullptr, X, codes, nullptr, scales, nullptr, rows, C, dt, code, (hipStream_t)hip_stream);
+    const dim3 grid(la::rows_blocks(rows, C)), block(256);
+    const hipStream_t st = (hipStream_t)hip_stream;
+    const uint8_t *c = (const uint8_t *)codes, *p = (const uint8_t *)scales;
+    if (dt == LA_F32) la::k_unpack<float><<<grid, block, 0, st>>>(c, p, (float *)X, rows, C, code == LA_I8);
+    else la::k_unpack<la::bf16_t><<<grid, block, 0, st>>>(c, p, (la::bf16_t *)X, rows, C, code == LA_I8);
+    return la::done();
 }
 
 size_t la_rmsnorm_workspace_bytes(size_t rows, int C)
