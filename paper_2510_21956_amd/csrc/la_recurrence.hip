@@ -100,7 +100,7 @@ struct Walk {
     const int *lengths;
     uint64_t *sums, *states;  // [B, tiles, C] words (P, q); [B, blocks, C] words (state, 0)
     unsigned *ticket;
-    int B, N, C, groups, tiles, blocks, span, lots;
+    int B, N, C, lanes, groups, chains, tiles, blocks, span, lots;
 };
 constexpr uint32_t kNothing = 0xffffffffu;
 constexpr int kMostSpan = 32, kLots = 8, kCounters = kLots * 64;
@@ -134,7 +134,8 @@ __device__ __forceinline__ uint64_t await(const uint64_t *p, uint64_t word)
 // of a sequence that have rows as the walk meets them.
 template <bool BWD>
 struct Place {
-    unsigned c;
+    unsigned at;  // of this lane's channels, from the address of row t of sequence b on
+    int c, own;   // its first channel, its sequence
     int b, n, r0, end, count, tile, tiles, order;
     bool goes_on;  // there is a tile after it
     // the s-th row of the walk through the tile (its last one for s behind it)
@@ -148,10 +149,15 @@ template <int V, int ROWS, bool BWD>
 __device__ __forceinline__ Place<BWD> place_of(const Walk &a, unsigned k, unsigned chain, int lane)
 {
     Place<BWD> p;
-    p.b = __builtin_amdgcn_readfirstlane(chain / a.groups);
+    const int together = 64 / a.lanes;  // narrow sequences that share a wave, all of one length
+    p.b = __builtin_amdgcn_readfirstlane(chain / a.groups * together);
     p.tile = __builtin_amdgcn_readfirstlane(BWD ? a.tiles - 1 - (int)k : (int)k);
-    // the lanes behind the last channel take the last V channels once more: they write what their neighbour writes
-    p.c = (unsigned)min(((int)chain - p.b * a.groups) * 64 * V + lane * V, a.C - V);
+    // the lanes behind the last channel take the last V channels once more, those behind the last sequence that
+    // one: they write what their neighbour writes
+    const int other = min(lane / a.lanes, a.B - 1 - p.b);
+    p.c = min(((int)(chain % a.groups) * 64 + lane % a.lanes) * V, a.C - V);
+    p.own = p.b + other;
+    p.at = (unsigned)other * (unsigned)a.N * (unsigned)a.C + p.c;
     p.n = __builtin_amdgcn_readfirstlane(rows_of(a, p.b));
     p.r0 = p.tile * ROWS;
     p.end = min(a.N, p.r0 + ROWS);
@@ -172,10 +178,10 @@ struct Rows {
         size_t o = ((size_t)p.b * a.N + t) * a.C;  // the same in all lanes
 #pragma unroll
         for (int i = 0; i < R; ++i) {
-            g[i] = request<T, V>((const T *)a.Gate + o, p.c);
-            if (BWD) d[i] = request<T, V>((const T *)a.dH + o, p.c);
-            if (!BWD || GATE == LA_GATE_SIGMOID) x[i] = request<T, V>((const T *)a.X + o, p.c);
-            if (BWD) h[i] = request<T, V>((const T *)a.H + (t ? o - a.C : o), p.c);
+            g[i] = request<T, V>((const T *)a.Gate + o, p.at);
+            if (BWD) d[i] = request<T, V>((const T *)a.dH + o, p.at);
+            if (!BWD || GATE == LA_GATE_SIGMOID) x[i] = request<T, V>((const T *)a.X + o, p.at);
+            if (BWD) h[i] = request<T, V>((const T *)a.H + (t ? o - a.C : o), p.at);
             if (first + i + 1 < p.count) {  // behind the tile's last row: that row once more
                 o = BWD ? o - a.C : o + a.C;
                 t += BWD ? -1 : 1;
@@ -193,7 +199,7 @@ __global__ void __launch_bounds__(W * 64, 4) k_walk(Walk a)
     constexpr int ROWS = W * R;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, first = wave * R;
     // every lot's counter hands out the tiles of its own chains, neighbouring ones
-    const unsigned chains = (unsigned)a.B * a.groups, lot = blockIdx.x % a.lots, per = (chains + a.lots - 1) / a.lots;
+    const unsigned chains = (unsigned)a.chains, lot = blockIdx.x % a.lots, per = (chains + a.lots - 1) / a.lots;
     const unsigned mine = lot * per < chains ? min(per, chains - lot * per) : 0;
     unsigned k = blockIdx.x / a.lots;
     if (a.tiles > 1) {
@@ -211,15 +217,15 @@ __global__ void __launch_bounds__(W * 64, 4) k_walk(Walk a)
     for (int j = 0; j < V; ++j) P[j] = 1.f, q[j] = e[j] = 0.f;
     for (int t = max(p.r0, p.n) + wave; t < p.end; t += W) {  // padding
         const size_t o = ((size_t)p.b * a.N + t) * a.C;
-        leave<T, V>(O0 + o, p.c, q);
-        if (BWD) leave<T, V>(O1 + o, p.c, q);
+        leave<T, V>(O0 + o, p.at, q);
+        if (BWD) leave<T, V>(O1 + o, p.at, q);
     }
     if (a.first) {
-        const Cells<float, V> s = request<float, V>(a.first + (size_t)p.b * a.C, p.c);
+        const Cells<float, V> s = request<float, V>(a.first + (size_t)p.own * a.C, p.c);
 #pragma unroll
         for (int j = 0; j < V; ++j) e[j] = s.at(j);
     }
-    if (p.n == 0 && p.tile == 0 && wave == 0 && a.last) leave<float, V>(a.last + (size_t)p.b * a.C, p.c, e);
+    if (p.n == 0 && p.tile == 0 && wave == 0 && a.last) leave<float, V>(a.last + (size_t)p.own * a.C, p.c, e);
     if (p.count <= 0) return;
 #pragma unroll
     for (int i = 0; i < R; ++i) {
@@ -253,19 +259,19 @@ __global__ void __launch_bounds__(W * 64, 4) k_walk(Walk a)
             }
             if (p.goes_on && !ends) {
                 const uint32_t bits = __float_as_uint(P[j]);
-                publish(a.sums + ((size_t)p.b * a.tiles + p.tile) * a.C + p.c + j, bits == kNothing ? 0x7fc00000u : bits, q[j]);
+                publish(a.sums + ((size_t)p.own * a.tiles + p.tile) * a.C + p.c + j, bits == kNothing ? 0x7fc00000u : bits, q[j]);
             }
         }
     }
     if (p.order > 0) {
-        const uint64_t *from = a.states + ((size_t)p.b * a.blocks + block - 1) * a.C + p.c;
+        const uint64_t *from = a.states + ((size_t)p.own * a.blocks + block - 1) * a.C + p.c;
         uint64_t word[V];
         const bool last_wave = block > 0 && wave == W - 1;
         if (last_wave)
 #pragma unroll
             for (int j = 0; j < V; ++j) word[j] = peek(from + j);
         for (int s = start + wave; s < p.order; s += W) {
-            const uint64_t *f = a.sums + ((size_t)p.b * a.tiles + (BWD ? p.tiles - 1 - s : s)) * a.C + p.c;
+            const uint64_t *f = a.sums + ((size_t)p.own * a.tiles + (BWD ? p.tiles - 1 - s : s)) * a.C + p.c;
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 const uint64_t w = await(f + j, peek(f + j));
@@ -285,7 +291,7 @@ __global__ void __launch_bounds__(W * 64, 4) k_walk(Walk a)
             e[j] = y.x * e[j] + y.y;
         }
         if (wave == 0 && ends && p.goes_on)
-            publish(a.states + ((size_t)p.b * a.blocks + block) * a.C + p.c + j, 0, P[j] * e[j] + q[j]);
+            publish(a.states + ((size_t)p.own * a.blocks + block) * a.C + p.c + j, 0, P[j] * e[j] + q[j]);
         for (int v = 0; v < wave; ++v) {
             const float2 y = sums[v][lane * V + j];
             e[j] = y.x * e[j] + y.y;
@@ -305,7 +311,7 @@ __global__ void __launch_bounds__(W * 64, 4) k_walk(Walk a)
                 } else {
                     const float d = u[i][j] + e[j];
                     float prev = r.h[i].at(j);
-                    if (t == 0) prev = a.h0 ? a.h0[(size_t)p.b * a.C + p.c + j] : 0.f;
+                    if (t == 0) prev = a.h0 ? a.h0[(size_t)p.own * a.C + p.c + j] : 0.f;
                     e[j] = f[i][j] * d;
                     if (GATE == LA_GATE_SIGMOID) {
                         o0[j] = rest[i][j] * d;
@@ -316,13 +322,13 @@ __global__ void __launch_bounds__(W * 64, 4) k_walk(Walk a)
                     }
                 }
             }
-            leave<T, V, BWD>(O0 + o, p.c, o0);
-            if (BWD) leave<T, V, BWD>(O1 + o, p.c, o1);
+            leave<T, V, BWD>(O0 + o, p.at, o0);
+            if (BWD) leave<T, V, BWD>(O1 + o, p.at, o1);
             o = BWD ? o - a.C : o + a.C;
             t += BWD ? -1 : 1;
         }
     // the wave with the last row of the walk
-    if (a.last && !p.goes_on && first < p.count && first + R >= p.count) leave<float, V>(a.last + (size_t)p.b * a.C, p.c, e);
+    if (a.last && !p.goes_on && first < p.count && first + R >= p.count) leave<float, V>(a.last + (size_t)p.own * a.C, p.c, e);
 }
 
 // The counter at zero, the words of `n` 16-byte units behind it at kNothing.
@@ -353,7 +359,7 @@ __global__ void __launch_bounds__(256) k_step(const T *X, const T *G, T *H, floa
 
 // How a call is tiled.
 struct Tiling {
-    int V, W, groups, tiles, blocks, span, lots;
+    int V, W, lanes, groups, chains, tiles, blocks, span, lots;
     size_t words, bytes;  // 16-byte units of published words; the workspace
 };
 
@@ -368,12 +374,20 @@ struct Tiling {
 // sides, us: one sequence of 100000 rows, bf16, 2048 channels, forward, W = 16, lots 1, span 4 241; W = 8 301;
 // lots 8 277; 128 channels, span 32 54, span 8 80; 8 x 500 rows of 3200 channels, fp32, W = 8, lots 8 27; W = 16 32;
 // lots 1 35.
-Tiling tiling(int B, int N, int C, la_dtype dt, bool backward)
+//
+// Narrow sequences, heads of a head layout: up to 64 channels a lane takes one of bfloat16 too (64 sequences of 4096
+// rows of 64, backward, 48 us; two a lane 63), and several sequences share a wave where none ends before the others
+// (1000 of 300 rows of 16, bf16, forward, one a wave 34 us, four 14).
+Tiling tiling(int B, int N, int C, la_dtype dt, bool backward, bool ragged)
 {
     Tiling p;
-    p.V = dt == LA_BF16 && C >= 2 ? 2 : 1;
+    p.V = dt == LA_BF16 && C > 64 ? 2 : 1;
     p.groups = (C + 64 * p.V - 1) / (64 * p.V);
-    const long chains = (long)B * p.groups;
+    p.lanes = 64;
+    // (the lanes' offsets are 32 bits)
+    while (!ragged && C <= p.lanes / 2 && 64 / p.lanes < B && p.lanes > 4 && (double)N * C * 128 / p.lanes < 1 << 28) p.lanes /= 2;
+    const long chains = (long)((B + 64 / p.lanes - 1) / (64 / p.lanes)) * p.groups;
+    p.chains = (int)chains;
     const int R = backward ? kRowsBack : kRowsFwd, eights = (N + 8 * R - 1) / (8 * R);
     p.W = eights <= 2 || (eights > 24 && chains < 32) || eights > 100 ? 16 : 8;
     p.lots = chains < 16 || eights > 100 ? 1 : kLots;
@@ -399,7 +413,7 @@ template <typename T, int V, int GATE, bool BWD>
 void launch(const Walk &w, const Tiling &p, hipStream_t st)
 {
     constexpr int R = BWD ? kRowsBack : kRowsFwd;
-    const size_t chains = (size_t)w.B * w.groups, most = (chains + w.lots - 1) / w.lots * w.lots * w.tiles;
+    const size_t chains = w.chains, most = (chains + w.lots - 1) / w.lots * w.lots * w.tiles;
     if (w.tiles > 1)
         k_clear<<<dim3((unsigned)((p.words + 255) / 256)), dim3(256), 0, st>>>(w.ticket, (uint4 *)w.sums, p.words);
     if (p.W == 8) k_walk<T, V, GATE, BWD, 8, R><<<dim3((unsigned)most), dim3(512), 0, st>>>(w);
@@ -408,7 +422,7 @@ void launch(const Walk &w, const Tiling &p, hipStream_t st)
 template <bool BWD>
 la_status run(Walk w, const Tiling &p, void *ws, la_gate gate, la_dtype dt, hipStream_t st)
 {
-    w.groups = p.groups, w.tiles = p.tiles, w.blocks = p.blocks, w.span = p.span, w.lots = p.lots;
+    w.lanes = p.lanes, w.groups = p.groups, w.chains = p.chains, w.tiles = p.tiles, w.blocks = p.blocks, w.span = p.span, w.lots = p.lots;
     w.ticket = (unsigned *)ws;
     w.sums = (uint64_t *)((char *)ws + kCounters);
     w.states = w.sums + (size_t)w.B * w.C * w.tiles;
@@ -434,7 +448,9 @@ extern "C" {
 size_t la_recurrence_workspace_bytes(int B, int N, int C, la_dtype dt, int is_backward)
 {
     if (la::check_shape(B, N, C, LA_GATE_VALUE, dt) != LA_OK) return 0;
-    return la::tiling(B, N, C, dt, is_backward).bytes;
+    // a call with lengths may be tiled in another way than one without
+    const size_t a = la::tiling(B, N, C, dt, is_backward, false).bytes, b = la::tiling(B, N, C, dt, is_backward, true).bytes;
+    return a > b ? a : b;
 }
 
 la_status la_recurrence_forward(const void *X, const void *Gate, const float *h0, void *Hs, float *last,
@@ -449,8 +465,8 @@ la_status la_recurrence_forward(const void *X, const void *Gate, const float *h0
         if (!la::aligned_to(p, e)) return LA_ERR_ALIGN;
     for (const void *p : {(const void *)h0, (const void *)last, (const void *)lengths})
         if (!la::aligned_to(p, 4)) return LA_ERR_ALIGN;
-    const la::Tiling p = la::tiling(B, N, C, dt, false);
-    if (la::bad_workspace(workspace, workspace_bytes, p.bytes)) return LA_ERR_WORKSPACE;
+    const la::Tiling p = la::tiling(B, N, C, dt, false, lengths != nullptr);
+    if (la::bad_workspace(workspace, workspace_bytes, la_recurrence_workspace_bytes(B, N, C, dt, 0))) return LA_ERR_WORKSPACE;
     const la::Range ins[] = {{X, tb}, {Gate, tb}, {h0, sb}, {lengths, (size_t)B * 4}};
     const la::Range outs[] = {{Hs, tb}, {last, sb}, {workspace, p.bytes}};
     if (la::any_alias(ins, 4, outs, 3)) return LA_ERR_ALIAS;
@@ -474,8 +490,8 @@ la_status la_recurrence_backward(const void *X, const void *Gate, const float *h
         if (!la::aligned_to(p, e)) return LA_ERR_ALIGN;
     for (const void *p : {(const void *)h0, (const void *)dlast, (const void *)dh0, (const void *)lengths})
         if (!la::aligned_to(p, 4)) return LA_ERR_ALIGN;
-    const la::Tiling p = la::tiling(B, N, C, dt, true);
-    if (la::bad_workspace(workspace, workspace_bytes, p.bytes)) return LA_ERR_WORKSPACE;
+    const la::Tiling p = la::tiling(B, N, C, dt, true, lengths != nullptr);
+    if (la::bad_workspace(workspace, workspace_bytes, la_recurrence_workspace_bytes(B, N, C, dt, 1))) return LA_ERR_WORKSPACE;
     const la::Range ins[] = {{X, tb}, {Gate, tb}, {h0, sb}, {Hs, tb}, {dHs, tb}, {dlast, sb}, {lengths, (size_t)B * 4}};
     const la::Range outs[] = {{dX, tb}, {dGate, tb}, {dh0, sb}, {workspace, p.bytes}};
     if (la::any_alias(ins, 7, outs, 4)) return LA_ERR_ALIAS;

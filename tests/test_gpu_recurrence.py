@@ -73,6 +73,27 @@ def test_against_the_definition(B, N, C, gate, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,N,C", [(65, 300, 16), (5, 500, 20), (3, 1500, 32), (2, 129, 8), (33, 17, 5), (9, 400, 4), (7, 257, 64)])
+def test_heads_that_share_a_wave(B, N, C, dtype):
+    """Narrow sequences side by side in a wave, some waves not full; the same with lengths, which take a wave each."""
+    x, g, h0, dh, dlast = draw(B, N, C, dtype, "sigmoid", B + N + C)
+    h, last = forward(*up(x, g, h0), None, "sigmoid")
+    want, wlast, E, Elast = recurrence64(x, g, h0, None, "sigmoid")
+    within(h, want, E, x.dtype)
+    within(last, wlast, Elast, torch.float32)
+    n = torch.full((B,), N, dtype=torch.int32)
+    h2, last2 = forward(*up(x, g, h0), n.cuda(), "sigmoid")
+    within(h2, want, E, x.dtype)
+    within(last2, wlast, Elast, torch.float32)
+    stored = want.to(x.dtype)
+    ref = recurrence_backward64(x, g, h0, stored, dh, dlast, None, "sigmoid")
+    for lengths in (None, n.cuda()):
+        got = backward(*up(x, g, h0, stored, dh, dlast), lengths, "sigmoid")
+        for a, b, e, t in zip(got, ref[:3], ref[3:], (x.dtype, x.dtype, torch.float32)):
+            within(a, b, e, t)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("gate", ["value", "sigmoid"])
 @pytest.mark.parametrize("N,C,lengths", [(300, 65, [300, 0, 17, 1, 299]), (2500, 64, [1, 2500, 1300, 0, 40]), (40, 7, [0, 0, -3, 99, 5])])
 def test_padded_batches(N, C, lengths, gate, dtype):
