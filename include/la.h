@@ -421,7 +421,9 @@ LA_API la_status la_backward_traced(const void *Q, const void *K, const void *V,
  * A gate of zero (LA_GATE_SIGMOID: -infinity) starts anew: packed documents need no lengths.  The product
  * of a run of gates has to be a float (gates of magnitude up to 1 are); an infinity or a NaN spoils its
  * channel from its row on (backward: up to it), whatever the gates after it.
- * Limits: B, N, C >= 1, B*N*C < 2^40, B * ceil(C / 64) < 2^23 and, times ceil(N / 64), < 2^31.
+ * Calls that share a workspace must not overlap in time, two captured graphs' neither: workgroups of one
+ * call wait for words that others of it leave there.  (Such waits are bounded: the results are then NaN.)
+ * Limits: B, N, C >= 1, N <= 2^30, B*N*C < 2^40, B * ceil(C / 64) < 2^23 and, times ceil(N / 64), < 2^31.
  *
  * la_recurrence_step appends T rows to a carried state, [B, C] float32, and updates it in place: the
  * form for single tokens.  No workspace; rows are walked one after another, T is meant to be small.

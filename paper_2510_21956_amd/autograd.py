@@ -110,7 +110,7 @@ def linear_attention(Q, K, V, a=1.0, b=0.5, causal=True, normalize_qk=False, che
         code = _b.eight_bit_code(checkpoint)
         if Q.shape != K.shape or Q.shape != V.shape:
             raise ValueError("shape mismatch")
-        O = _b.in_native_code("checkpointed", "la_forward_save", Q, K, V, a, b, causal, normalize_qk, code)
+        O = _b.in_native_code("checkpointed", "la_forward_save" if normalize_qk else "la_forward", Q, K, V, a, b, causal, normalize_qk, code)
         if O is not None:
             return O
         return CheckpointedAttentionFunction.apply(Q, K, V, a, b, causal, normalize_qk, code)

@@ -231,7 +231,7 @@ static AbLayout ab_layout(const Plan &bwd, size_t T, int D, la_dtype dt, bool fa
 
 extern "C" {
 
-int la_version(void) { return 200; }
+int la_version(void) { return 210; }
 
 const char *la_status_string(la_status s)
 {

@@ -103,6 +103,7 @@ struct Walk {
     int B, N, C, lanes, groups, chains, tiles, blocks, span, lots;
 };
 constexpr uint32_t kNothing = 0xffffffffu;
+constexpr int kMostLooks = 1 << 21;
 constexpr int kMostSpan = 32, kLots = 8, kCounters = kLots * 64;
 
 __device__ __forceinline__ int rows_of(const Walk &w, int b)
@@ -120,10 +121,12 @@ __device__ __forceinline__ uint64_t peek(const uint64_t *p)
 {
     return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
-// A word that was peeked at, once it is there.
+// A word that was peeked at, once it is there.  Within one call every wait ends (above) in microseconds; where two calls
+// overlap on one workspace, against the rules, one may wipe out what the other waits for: after some seconds of looking
+// a wait ends with what is there, ones, which are NaN in either half and spoil the results.
 __device__ __forceinline__ uint64_t await(const uint64_t *p, uint64_t word)
 {
-    while ((uint32_t)(word >> 32) == kNothing) {
+    for (int looks = 0; (uint32_t)(word >> 32) == kNothing && looks < kMostLooks; ++looks) {
         __builtin_amdgcn_s_sleep(1);
         word = peek(p);
     }
@@ -199,9 +202,10 @@ __global__ void __launch_bounds__(W * 64, 4) k_walk(Walk a)
     constexpr int ROWS = W * R;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64, first = wave * R;
     // every lot's counter hands out the tiles of its own chains, neighbouring ones
-    const unsigned chains = (unsigned)a.chains, lot = blockIdx.x % a.lots, per = (chains + a.lots - 1) / a.lots;
+    const unsigned group = blockIdx.y * gridDim.x + blockIdx.x;
+    const unsigned chains = (unsigned)a.chains, lot = group % a.lots, per = (chains + a.lots - 1) / a.lots;
     const unsigned mine = lot * per < chains ? min(per, chains - lot * per) : 0;
-    unsigned k = blockIdx.x / a.lots;
+    unsigned k = group / a.lots;
     if (a.tiles > 1) {
         if (threadIdx.x == 0) ticket = atomicAdd(a.ticket + 16 * lot, 1u);
         block_sync();
@@ -401,7 +405,7 @@ Tiling tiling(int B, int N, int C, la_dtype dt, bool backward, bool ragged)
 
 la_status check_shape(int B, int N, int C, la_gate gate, la_dtype dt)
 {
-    if (B < 1 || N < 1 || C < 1) return LA_ERR_SHAPE;
+    if (B < 1 || N < 1 || C < 1 || N > 1 << 30) return LA_ERR_SHAPE;
     if (!real_type(dt) || (gate != LA_GATE_VALUE && gate != LA_GATE_SIGMOID)) return LA_ERR_UNSUPPORTED;
     if ((double)B * N * C >= 1099511627776.0) return LA_ERR_SHAPE;          // 2^40
     if ((double)B * ((C + 63) / 64) >= 8388608.0) return LA_ERR_SHAPE;  // 2^23
@@ -416,8 +420,10 @@ void launch(const Walk &w, const Tiling &p, hipStream_t st)
     const size_t chains = w.chains, most = (chains + w.lots - 1) / w.lots * w.lots * w.tiles;
     if (w.tiles > 1)
         k_clear<<<dim3((unsigned)((p.words + 255) / 256)), dim3(256), 0, st>>>(w.ticket, (uint4 *)w.sums, p.words);
-    if (p.W == 8) k_walk<T, V, GATE, BWD, 8, R><<<dim3((unsigned)most), dim3(512), 0, st>>>(w);
-    else k_walk<T, V, GATE, BWD, 16, R><<<dim3((unsigned)most), dim3(1024), 0, st>>>(w);
+    constexpr size_t wide = 1 << 21;  // a grid has less than 2^32 threads in a dimension
+    const dim3 grid((unsigned)(most < wide ? most : wide), (unsigned)((most + wide - 1) / wide));
+    if (p.W == 8) k_walk<T, V, GATE, BWD, 8, R><<<grid, dim3(512), 0, st>>>(w);
+    else k_walk<T, V, GATE, BWD, 16, R><<<grid, dim3(1024), 0, st>>>(w);
 }
 template <bool BWD>
 la_status run(Walk w, const Tiling &p, void *ws, la_gate gate, la_dtype dt, hipStream_t st)

@@ -106,7 +106,7 @@ def test_recurrence_refusals(lib):
     def step(X=p[0], G=p[1], H=p[2], S=p[7], B=2, T=1, C=65, gate=1, dt=1):
         return lib.la_recurrence_step(X, G, H, S, B, T, C, gate, dt, None)
     for call in (fwd, bwd):
-        for bad in ({"B": 0}, {"N": 0}, {"C": -1}, {"B": 1 << 20, "N": 1 << 20}, {"B": 1 << 23, "N": 1, "C": 1}):
+        for bad in ({"B": 0}, {"N": 0}, {"C": -1}, {"B": 1 << 20, "N": 1 << 20}, {"B": 1 << 23, "N": 1, "C": 1}, {"N": (1 << 30) + 1, "B": 1, "C": 1}):
             assert call(**bad) == SHAPE, bad
         for bad in ({"dt": 2}, {"dt": 7}, {"gate": 2}, {"gate": -1}):
             assert call(**bad) == UNSUPPORTED, bad
