@@ -106,10 +106,12 @@ constexpr uint32_t kNothing = 0xffffffffu;
 constexpr int kMostLooks = 1 << 21;
 constexpr int kMostSpan = 32, kLots = 8, kCounters = kLots * 64;
 
-__device__ __forceinline__ int rows_of(const Walk &w, int b)
+// Rows of sequence b.  `held`: the length of sequence `lane`, where a wave holds all of them: asked for before the wave
+// knows which one is its own.
+__device__ __forceinline__ int rows_of(const Walk &w, int b, int held)
 {
     if (!w.lengths) return w.N;
-    const int n = w.lengths[b];
+    const int n = w.B <= 64 ? __builtin_amdgcn_readlane(held, b) : __builtin_amdgcn_readfirstlane(w.lengths[b]);
     return n < 0 ? 0 : n > w.N ? w.N : n;
 }
 
@@ -149,7 +151,7 @@ struct Place {
     }
 };
 template <int V, int ROWS, bool BWD>
-__device__ __forceinline__ Place<BWD> place_of(const Walk &a, unsigned k, unsigned chain, int lane)
+__device__ __forceinline__ Place<BWD> place_of(const Walk &a, unsigned k, unsigned chain, int lane, int held)
 {
     Place<BWD> p;
     const int together = 64 / a.lanes;  // narrow sequences that share a wave, all of one length
@@ -161,7 +163,7 @@ __device__ __forceinline__ Place<BWD> place_of(const Walk &a, unsigned k, unsign
     p.c = min(((int)(chain % a.groups) * 64 + lane % a.lanes) * V, a.C - V);
     p.own = p.b + other;
     p.at = (unsigned)other * (unsigned)a.N * (unsigned)a.C + p.c;
-    p.n = __builtin_amdgcn_readfirstlane(rows_of(a, p.b));
+    p.n = rows_of(a, p.b, held);
     p.r0 = p.tile * ROWS;
     p.end = min(a.N, p.r0 + ROWS);
     p.count = min(p.n, p.end) - p.r0;
@@ -206,13 +208,14 @@ __global__ void __launch_bounds__(W * 64, 4) k_walk(Walk a)
     const unsigned chains = (unsigned)a.chains, lot = group % a.lots, per = (chains + a.lots - 1) / a.lots;
     const unsigned mine = lot * per < chains ? min(per, chains - lot * per) : 0;
     unsigned k = group / a.lots;
+    const int held = a.lengths && a.B <= 64 ? a.lengths[min(lane, a.B - 1)] : 0;
     if (a.tiles > 1) {
         if (threadIdx.x == 0) ticket = atomicAdd(a.ticket + 16 * lot, 1u);
         block_sync();
         k = __builtin_amdgcn_readfirstlane(ticket);
     }
     if (k >= mine * a.tiles) return;
-    const Place<BWD> p = place_of<V, ROWS, BWD>(a, k / mine, lot * per + k % mine, lane);
+    const Place<BWD> p = place_of<V, ROWS, BWD>(a, k / mine, lot * per + k % mine, lane, held);
     T *O0 = (T *)a.out0, *O1 = (T *)a.out1;
     Rows<T, V, GATE, BWD, R> r;
     if (p.count > 0) r.load(a, p, first);

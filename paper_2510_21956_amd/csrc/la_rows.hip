@@ -237,23 +237,26 @@ __global__ void __launch_bounds__(Share<L>::NT) k_norm_back(NormBack a)
     }
 }
 
-// dw from its shares: 64 channels a workgroup, sixteen runs of shares side by side.
+// dw from its shares, in a fixed order: sixteen channels a workgroup, whose 64 groups of lanes take a run of shares
+// each (1024 shares of 2048 channels: 5.2 us, 7.0 with 64 channels and 16 runs).
 __global__ void __launch_bounds__(1024) k_norm_join(const float *parts, float *dW, int n, int C)
 {
-    __shared__ float lds[16][64];
-    const int lane = threadIdx.x % 64, run = threadIdx.x / 64, c = blockIdx.x * 64 + lane;
-    const int per = (n + 15) / 16, end = min(n, (run + 1) * per);
+    __shared__ float lds[64][16];
+    const int channel = threadIdx.x % 16, run = threadIdx.x / 16, c = blockIdx.x * 16 + channel;
+    const int per = (n + 63) / 64, end = min(n, (run + 1) * per);
     float s = 0.f;
     if (c < C)
-#pragma unroll 4
+#pragma unroll 8
         for (int i = run * per; i < end; ++i) s += parts[(size_t)i * C + c];
-    lds[run][lane] = s;
+    lds[run][channel] = s;
     block_sync();
-    if (run == 0 && c < C) {
+    if (run < 4) {  // one wave
         s = 0.f;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s += lds[r][lane];
-        dW[c] = s;
+        for (int r = 0; r < 16; ++r) s += lds[run * 16 + r][channel];
+        s += __shfl_xor(s, 16);
+        s += __shfl_xor(s, 32);
+        if (run == 0 && c < C) dW[c] = s;
     }
 }
 
@@ -485,7 +488,7 @@ la_status la_rmsnorm_backward(const void *S, const void *Sscale, const void *W, 
                 <<<dim3(blocks), dim3(shape.lanes()), 0, stream>>>(a);
         });
     });
-    if (dW) la::k_norm_join<<<dim3((C + 63) / 64), dim3(1024), 0, stream>>>((const float *)workspace, dW, blocks, C);
+    if (dW) la::k_norm_join<<<dim3((C + 15) / 16), dim3(1024), 0, stream>>>((const float *)workspace, dW, blocks, C);
     return la::done();
 }
 

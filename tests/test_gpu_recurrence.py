@@ -216,6 +216,41 @@ def test_runs_repeat_bit_for_bit_and_streams_are_taken():
     assert all(torch.equal(a, b) for a, b in zip(back, back2))
 
 
+def test_many_padded_sequences():
+    """More sequences than a wave holds lengths of."""
+    B, N, C = 70, 200, 66
+    x, g, h0, dh, dlast = draw(B, N, C, "f32", "sigmoid", 13)
+    n = (torch.arange(B) * 7 % (N + 9) - 4).to(torch.int32)
+    h, last = forward(*up(x, g, h0), n.cuda(), "sigmoid")
+    want, wlast, E, Elast = recurrence64(x, g, h0, n, "sigmoid")
+    within(h, want, E, x.dtype)
+    within(last, wlast, Elast, torch.float32)
+    got = backward(*up(x, g, h0, want.float(), dh, dlast), n.cuda(), "sigmoid")
+    ref = recurrence_backward64(x, g, h0, want.float(), dh, dlast, n, "sigmoid")
+    for a, b, e in zip(got, ref[:3], ref[3:]):
+        within(a, b, e, torch.float32)
+
+
+def test_calls_side_by_side():
+    """Calls on two streams at once, each with a workspace of its own, give the bits of calls that run alone."""
+    sets = [up(*draw(1, 20000, 512, "bf16", "sigmoid", 14 + k)) for k in range(2)]
+    alone = []
+    for x, g, h0, dh, dlast in sets:
+        h, last = forward(x, g, h0, None, "sigmoid")
+        alone.append([h, last, *backward(x, g, h0, h, dh, dlast, None, "sigmoid")])
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for turn in range(5):
+        for k, (x, g, h0, dh, dlast) in enumerate(sets):
+            with torch.cuda.stream(streams[k]):
+                h, last = forward(x, g, h0, None, "sigmoid")
+                got[k] = [h, last, *backward(x, g, h0, h, dh, dlast, None, "sigmoid")]
+    torch.cuda.synchronize()
+    for a, b in zip(alone, got):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
 @pytest.mark.parametrize("N", [1, 30, 3000])
 def test_captured_calls(N):
     """Two graphs that share a workspace, replayed in turn on new inputs with eager calls in between; every
