@@ -8,8 +8,9 @@
 // before left, and the block's last tile publishes the state for the next.  So sums are joined in a fixed order
 // (two runs give the same bits), and only every span-th tile waits for a chain of states.
 //
-// A wave more than W does the joining: loads return in order, and the W waves have those of the next tile in
-// flight while it waits for published words.
+// Bound by HBM: forward 3 elements moved a row and channel, backward 5 or 6.  One sequence of 131072 rows, bf16, 2048
+// channels, sigmoid gates: forward 312 us (5.2 TB/s), backward 660 (4.9); short calls by the clearing launch
+// and a chain of tiles (2 x 3001 rows, 22 us; 3 x 5003 rows of 771 channels, 25 and 44, half the rate).
 //
 // Tiles are handed out by a counter, in an order in which a tile waits for earlier ones only: those are done or in
 // hand of a workgroup that waits for still earlier ones at most, whatever the order in which workgroups
