@@ -548,7 +548,18 @@ def _real_code(t):
     return LA_F32 if t.dtype == torch.float32 else LA_BF16
 
 
+_INTS = 1 << 31  # what the library's sizes stay below; ctypes would cut larger ones off
+
+
+def _fit(**sizes):
+    for name, n in sizes.items():
+        if n >= _INTS:
+            raise ValueError("%s must be less than 2^31, got %d" % (name, n))
+
+
 def la_recurrence_workspace_bytes(B, N, C, dt, is_backward):
+    if max(B, N, C) >= _INTS:
+        return 0
     return int(load_library().la_recurrence_workspace_bytes(B, N, C, dt, int(bool(is_backward))))
 
 
@@ -560,7 +571,9 @@ def _sequences(x, **states):
     for name, t in states.items():
         if t is not None and (t.shape != x.shape[:-2] + x.shape[-1:] or t.dtype != torch.float32):
             raise ValueError("%s must be float32 %s" % (name, tuple(x.shape[:-2] + x.shape[-1:])))
-    return (x.numel() // (N * C) if x.numel() else 0), N, C
+    B = x.numel() // (N * C) if x.numel() else 0
+    _fit(B=B, N=N, C=C)
+    return B, N, C
 
 
 def _lengths_ptr(lengths, x):
@@ -636,6 +649,7 @@ def _rows(x):
     if x.dim() < 1:
         raise ValueError("rows of [..., C] are needed")
     C = x.shape[-1]
+    _fit(C=C)
     return (x.numel() // C if x.numel() else 0), C
 
 
@@ -674,6 +688,8 @@ def la_unpack_rows(codes, scales, x, code, stream=None):
 
 
 def la_rmsnorm_workspace_bytes(rows, C):
+    if C >= _INTS:
+        return 0
     return int(load_library().la_rmsnorm_workspace_bytes(rows, C))
 
 

@@ -93,6 +93,12 @@ PyObject *tuple(const variable_list &ts)
 
 // ---- gated recurrence -----------------------------------------------------------------------------------------
 
+// Sizes that are the library's ints.
+bool ints(std::initializer_list<int64_t> sizes)
+{
+    return std::max(sizes) < (int64_t)1 << 31;
+}
+
 struct Sequences {
     int B, N, C;
     la_dtype dt;
@@ -102,6 +108,11 @@ struct Sequences {
         B = N && C ? (int)(x.numel() / N / C) : 0;
     }
 };
+bool ints_of_sequences(const at::Tensor &x)
+{
+    const int64_t N = x.size(-2), C = x.size(-1);
+    return ints({N, C, N && C ? x.numel() / N / C : 0});
+}
 std::vector<int64_t> state_sizes(const at::Tensor &x)
 {
     std::vector<int64_t> s(x.sizes().begin(), x.sizes().end() - 2);
@@ -178,7 +189,7 @@ PyObject *recurrence(PyObject *, PyObject *const *a, Py_ssize_t n)
     PyObject *declined = guarded(n, 5, [&]() -> PyObject * {
         if (!ours(a, 0, 3) || is_none(a[1]) || !PyLong_CheckExact(a[4])) Py_RETURN_NONE;
         const at::Tensor &x = tensor(a[0]);
-        require(x.dim() >= 2);
+        require(x.dim() >= 2 && ints_of_sequences(x));
         dtype_code(x);
         check_like(x, {a[1]});
         check_inputs(x, {a[0], a[1], a[2], a[3]});
@@ -204,7 +215,7 @@ PyObject *recurrence_step(PyObject *, PyObject *const *a, Py_ssize_t n)
         for (int i = 0; i < 4; ++i)
             if (!plain(a[i])) Py_RETURN_NONE;
         const at::Tensor &x = tensor(a[0]), &state = tensor(a[3]);
-        require(x.dim() >= 2 && PyLong_CheckExact(a[4]));
+        require(x.dim() >= 2 && ints_of_sequences(x) && PyLong_CheckExact(a[4]));
         check_packed({a[0], a[1], a[2], a[3]});
         check_like(x, {a[1], a[2]});
         dtype_code(x);
@@ -340,7 +351,7 @@ void check_norm(PyObject *x0, PyObject *weight, PyObject *residual)
 {
     require(plain(x0) && plain_or_none(weight) && plain_or_none(residual));
     const at::Tensor &x = tensor(x0);
-    require(x.dim() >= 1);
+    require(x.dim() >= 1 && ints({x.size(-1)}));
     dtype_code(x);
     check_like(x, {residual});
     check_inputs(x, {x0, weight, residual});

@@ -162,3 +162,19 @@ def test_captured_training_step():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_sizes_beyond_32_bits_are_refused():
+    """Sizes that a C int would cut off to ones the library takes: by both paths, before anything runs."""
+    big = (1 << 32) + 64
+    x = torch.empty(big, dtype=torch.bfloat16, device="cuda")
+    for s in ((1, big, 1), (big, 1, 1)):
+        v = x.view(*s)
+        with pytest.raises(ValueError, match="2\\^31"):
+            la.gated_recurrence(v, v)
+        with pytest.raises(ValueError, match="2\\^31"):
+            la.la_recurrence_step(v, v, v, torch.empty(s[0], 1, device="cuda"), la.LA_GATE_SIGMOID)
+    with pytest.raises(ValueError, match="2\\^31"):
+        la.rms_norm(x.view(1, big))
+    with pytest.raises(ValueError, match="2\\^31"):
+        la.rms_norm_quantised(x.view(1, big))

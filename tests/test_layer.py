@@ -221,6 +221,29 @@ def test_binding_refuses_other_shapes_and_types(lib):
             la.la_rmsnorm_backward(*a)
 
 
+def test_sizes_beyond_32_bits_are_refused(lib):
+    """Sizes that a C int would cut off to ones the library takes."""
+    D = lambda *s, t=torch.bfloat16: DeviceTensor(torch.empty(*s, dtype=t, device="meta"))
+    F, big = torch.float32, (1 << 32) + 64
+    for s in ((1, big, 1), (big, 1, 1), (1, 1, big)):
+        x, state = D(*s), D(s[0], s[2], t=F)
+        with pytest.raises(ValueError, match="2\\^31"):
+            la.la_recurrence_forward(x, x, None, x, state, None, 1, None)
+        with pytest.raises(ValueError, match="2\\^31"):
+            la.la_recurrence_backward(x, x, None, x, x, None, x, x, None, None, 1, None)
+        with pytest.raises(ValueError, match="2\\^31"):
+            la.la_recurrence_step(x, x, x, state, 1)
+        assert la.la_recurrence_workspace_bytes(*s, la.LA_BF16, 0) == 0
+    x, rs, powers, codes = D(1, big), D(1, t=F), D(1, big // 32, t=torch.uint8), D(1, big, t=torch.uint8)
+    for call in (lambda: la.la_pack_rows(x, codes, powers, la.LA_I8), lambda: la.la_unpack_rows(codes, powers, x, la.LA_I8),
+                 lambda: la.la_pack_tensors([x], [codes], [powers], la.LA_I8),
+                 lambda: la.la_rmsnorm_forward(x, None, None, x, None, None, None, None, rs, 1e-6),
+                 lambda: la.la_rmsnorm_backward(x, None, None, rs, x, None, x, None, None)):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
+    assert la.la_rmsnorm_workspace_bytes(1, big) == 0
+
+
 def test_wrappers_refuse_unknown_names():
     x = torch.zeros(2, 8, 16)
     for call in (lambda: la.gated_recurrence(x, x, gate="tanh"), lambda: la.rms_norm(x, checkpoint="int4"),
