@@ -2,7 +2,7 @@
 // small calls, in the manner of la_bind.cpp: plain tensors only; everything else, and whatever is to be refused,
 // stays with the Python functions of the same steps.  Through Python and here, us, nearly all of it host: rms_norm
 // on 5003 rows of 771, fp32, forward and backward 121 and 62; attention with checkpoints on 1 slice of 256 rows,
-// D = 16, 235 and 99; rms_norm_quantised on 8 rows 17 and 7.0; a step of a recurrence 8.3 and 4.0.
+// D = 16, 235 and 91; rms_norm_quantised on 8 rows 17 and 7.0; a step of a recurrence 8.3 and 4.0.
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
 
@@ -450,27 +450,27 @@ struct Checkpointed : torch::autograd::Function<Checkpointed> {
             const c10::DeviceGuard guard(dO.device());
             const int B = dO.size(0), H = dO.size(1), N = dO.size(2), D = dO.size(3);
             const size_t rows = (size_t)B * H * N;
-            const at::Tensor x = at::empty(codes.sizes(), dO.options()), O = at::empty_like(dO),
-                             G = at::empty({B, H, N}, dO.options().dtype(at::kFloat));
             for (int i = 0; i < 3; ++i) out[i] = at::empty_like(dO);
             // one workspace for both passes, which follow one another on the stream
             const size_t wb = std::max(att_bytes(B, H, N, D, dt, causal, 0), att_bytes(B, H, N, D, dt, causal, 1)),
-                         ns = att_saved_bytes(B, H, N, D, dt, causal);
-            const at::Tensor ws = buffer(wb, dO);
-            at::Tensor saved;
-            if (ns) saved = buffer(ns, dO);
-            const size_t sb = ns ? bytes(saved) : 0;
-            char *const q = (char *)x.data_ptr(), *const k = q + rows * D * x.element_size(), *const vv = k + rows * D * x.element_size();
-            float *const g = (float *)G.data_ptr();
+                         ns = att_saved_bytes(B, H, N, D, dt, causal), tb = rows * D * dO.element_size();
+            // Q, K, V side by side, O, g, the hand-over and the workspace in one allocation
+            const size_t sizes[] = {3 * tb, tb, rows * 4, ns, std::max(wb, (size_t)256)};
+            size_t at[5], total = 0;
+            for (int i = 0; i < 5; ++i) at[i] = total, total += (sizes[i] + 255) / 256 * 256;
+            const at::Tensor room = buffer(total, dO);
+            char *const base = (char *)room.data_ptr(), *const q = base, *const k = q + tb, *const vv = k + tb;
+            void *const O = base + at[1], *const saved = ns ? base + at[3] : nullptr, *const ws = base + at[4];
+            float *const g = (float *)(base + at[2]);
             void *const st = current_stream(dO);
             int rc = unpack_rows(codes.data_ptr(), powers.data_ptr(), q, 3 * rows, D, (la_dtype)code, dt, st);
             if (rc == 0)
-                rc = (norm ? att_save_qknorm : att_save)(q, k, vv, O.data_ptr(), g, B, H, N, D, (float)a, (float)b, causal, dt,
-                                                         ws.data_ptr(), bytes(ws), data(saved), sb, st, nullptr);
+                rc = (norm ? att_save_qknorm : att_save)(q, k, vv, O, g, B, H, N, D, (float)a, (float)b, causal, dt, ws, wb, saved,
+                                                         ns, st, nullptr);
             if (rc == 0)
                 rc = (norm ? att_backward_qknorm : att_backward)(
-                    q, k, vv, O.data_ptr(), g, dO.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), B, H, N,
-                    D, (float)a, (float)b, causal, dt, ws.data_ptr(), bytes(ws), data(saved), sb, st, nullptr);
+                    q, k, vv, O, g, dO.data_ptr(), out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), B, H, N, D, (float)a,
+                    (float)b, causal, dt, ws, wb, saved, ns, st, nullptr);
             if (rc == 0) return once(std::move(out), grads);
         }
         pybind11::gil_scoped_acquire gil;
