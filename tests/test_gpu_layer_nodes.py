@@ -1,5 +1,7 @@
 """The autograd nodes of the operators around the attention in native code and in Python: the same results, bit
 for bit, and the same refusals."""
+import threading
+
 import pytest
 import torch
 
@@ -162,6 +164,69 @@ def test_captured_training_step():
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def block(x, r, g, w, dy):
+    """Norm, attention with checkpoints, recurrence, norm into 8 bits, and the gradients."""
+    y, s = la.rms_norm(x, w, r, checkpoint="int8")
+    q = y.view(2, 300, 4, 32).transpose(1, 2)
+    o = la.linear_attention(q, q, q.flip(2), checkpoint="e4m3", normalize_qk=True)
+    h, last = la.gated_recurrence(o.transpose(1, 2).reshape(2, 300, 128), g)
+    eight = [t.view(torch.uint8) for t in la.rms_norm_quantised(h, w)]
+    return [h, last, s, *eight, *torch.autograd.grad([h, last, s], [x, r, g, w], [dy, last.detach(), dy])]
+
+
+def block_inputs(k):
+    return [t.requires_grad_(j < 4) for j, t in enumerate(
+        [rand(2, 300, 128, seed=10 * k + j, dtype=torch.bfloat16) for j in range(3)] + [1 + 0.1 * rand(128, seed=k)] +
+        [rand(2, 300, 128, seed=10 * k + 7, dtype=torch.bfloat16)])]
+
+
+def test_captured_block():
+    ins = block_inputs(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        block(*ins)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = block(*ins)
+    for k in (1, 2, 0, 1):
+        new = block_inputs(k)
+        with torch.no_grad():
+            for a, b in zip(ins, new):
+                a.copy_(b)
+        want = block(*new)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_threads_with_streams_of_their_own():
+    """Four threads at once give the bits of calls that run alone."""
+    sets = [block_inputs(k) for k in range(4)]
+    alone = [[t.detach() for t in block(*s)] for s in sets]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(10):
+                    got = block(*sets[k])
+                    torch.cuda.current_stream().synchronize()
+                    if not all(torch.equal(a, b) for a, b in zip(got, alone[k])):
+                        bad.append(k)
+        except Exception as e:
+            bad.append(e)
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
 
 
 def test_sizes_beyond_32_bits_are_refused():
