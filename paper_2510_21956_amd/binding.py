@@ -508,8 +508,9 @@ def la_backward_qknorm_saved(Q, K, V, O, G, dO, dQ, dK, dV, a, b, causal, worksp
 
 # ---- the operators around the attention ---------------------------------------------------------
 
-def _call(name, ref, stream, *args):
-    """Calls the entry point with the stream behind its arguments, on ref's device."""
+def _call(name, ref, stream, written, *args):
+    """Calls the entry point with the stream behind its arguments, on ref's device.  `written`: the tensors that it
+    writes, which autograd has to know of: a node that saved one of them must not go on with the new values."""
     f = getattr(load_library(), name)
     index = ref.get_device()
     if torch.cuda.current_device() == index:
@@ -519,6 +520,7 @@ def _call(name, ref, stream, *args):
             rc = f(*args, _stream_ptr(stream, ref))
     if rc != 0:
         raise LaError(rc, name)
+    torch.autograd.graph.increment_version([t for t in written if t is not None and not t.is_inference()])
 
 
 def _room(t):
@@ -592,7 +594,7 @@ def la_recurrence_forward(x, gates, h0, h, last, lengths, gate, workspace, strea
     _check_tensors(x, gates, h0, h, last, lengths, workspace)
     _like(x, gates=gates, h=h)
     B, N, C = _sequences(x, h0=h0, last=last)
-    _call("la_recurrence_forward", x, stream, _ptr(x), _ptr(gates), _ptr(h0), _ptr(h), _ptr(last),
+    _call("la_recurrence_forward", x, stream, (h, last), _ptr(x), _ptr(gates), _ptr(h0), _ptr(h), _ptr(last),
           _lengths_ptr(lengths, x), B, N, C, int(gate), _real_code(x), *_room(workspace))
 
 
@@ -602,13 +604,14 @@ def la_recurrence_backward(x, gates, h0, h, dh, dlast, dx, dgates, dh0, lengths,
     _check_tensors(x, gates, h0, h, dh, dlast, dx, dgates, dh0, lengths, workspace)
     _like(x, gates=gates, h=h, dh=dh, dx=dx, dgates=dgates)
     B, N, C = _sequences(x, h0=h0, dlast=dlast, dh0=dh0)
-    _call("la_recurrence_backward", x, stream, _ptr(x), _ptr(gates), _ptr(h0), _ptr(h), _ptr(dh), _ptr(dlast),
+    _call("la_recurrence_backward", x, stream, (dx, dgates, dh0), _ptr(x), _ptr(gates), _ptr(h0), _ptr(h), _ptr(dh), _ptr(dlast),
           _ptr(dx), _ptr(dgates), _ptr(dh0), _lengths_ptr(lengths, x), B, N, C, int(gate), _real_code(x),
           *_room(workspace))
 
 
 def la_recurrence_step(x, gates, h, state, gate, stream=None):
-    """la_recurrence_step of include/la.h: x, gates, h [..., T, C]; state [..., C] float32, updated in place."""
+    """la_recurrence_step of include/la.h: x, gates, h [..., T, C]; state [..., C] float32, updated in place (as a change
+    that autograd sees, and outside of any graph: a state with a history is left with that of its values before)."""
     if _native is not None:
         rc = _native.recurrence_step(x, gates, h, state, gate, stream)
         if rc == 0:
@@ -619,7 +622,8 @@ def la_recurrence_step(x, gates, h, state, gate, stream=None):
     _check_tensors(x, gates, h, state)
     _like(x, gates=gates, h=h)
     B, T, C = _sequences(x, state=state)
-    _call("la_recurrence_step", x, stream, _ptr(x), _ptr(gates), _ptr(h), _ptr(state), B, T, C, int(gate), _real_code(x))
+    _call("la_recurrence_step", x, stream, (h, state), _ptr(x), _ptr(gates), _ptr(h), _ptr(state), B, T, C, int(gate),
+          _real_code(x))
 
 
 LA_GROUP = 32  # neighbours of a row that share a power of two
@@ -660,7 +664,7 @@ def la_pack_rows(x, codes, scales, code, stream=None):
     _check_tensors(x, codes, scales)
     _eight(codes, scales, x, code, "packed")
     rows, C = _rows(x)
-    _call("la_pack_rows", x, stream, _ptr(x), _ptr(codes), _ptr(scales), rows, C, _real_code(x), int(code))
+    _call("la_pack_rows", x, stream, (codes, scales), _ptr(x), _ptr(codes), _ptr(scales), rows, C, _real_code(x), int(code))
 
 
 def la_pack_tensors(xs, codes, scales, code, stream=None):
@@ -675,7 +679,7 @@ def la_pack_tensors(xs, codes, scales, code, stream=None):
         _eight(c, s, x, code, "packed")
     rows, C = _rows(xs[0])
     lists = [(ctypes.c_void_p * len(ts))(*map(_ptr, ts)) for ts in (xs, codes, scales)]
-    _call("la_pack_tensors", xs[0], stream, len(xs), *lists, rows, C, _real_code(xs[0]), int(code))
+    _call("la_pack_tensors", xs[0], stream, (*codes, *scales), len(xs), *lists, rows, C, _real_code(xs[0]), int(code))
 
 
 def la_unpack_rows(codes, scales, x, code, stream=None):
@@ -684,7 +688,7 @@ def la_unpack_rows(codes, scales, x, code, stream=None):
     _check_tensors(x, codes, scales)
     _eight(codes, scales, x, code, "packed")
     rows, C = _rows(x)
-    _call("la_unpack_rows", x, stream, _ptr(codes), _ptr(scales), _ptr(x), rows, C, int(code), _real_code(x))
+    _call("la_unpack_rows", x, stream, (x,), _ptr(codes), _ptr(scales), _ptr(x), rows, C, int(code), _real_code(x))
 
 
 def la_rmsnorm_workspace_bytes(rows, C):
@@ -732,8 +736,8 @@ def la_rmsnorm_forward(x, residual, weight, y, yscales, total, kept, kscales, rs
         raise ValueError("kept and kscales need kcode")
     _per_row(x, rstd=rstd)
     rows, C = _rows(x)
-    _call("la_rmsnorm_forward", x, stream, _ptr(x), _ptr(residual), _ptr(weight), _ptr(y), _ptr(yscales), _ptr(total),
-          _ptr(kept), _ptr(kscales), _ptr(rstd), rows, C, float(eps), dt, wt, dt if ycode is None else int(ycode),
+    _call("la_rmsnorm_forward", x, stream, (y, yscales, total, kept, kscales, rstd), _ptr(x), _ptr(residual),
+          _ptr(weight), _ptr(y), _ptr(yscales), _ptr(total), _ptr(kept), _ptr(kscales), _ptr(rstd), rows, C, float(eps), dt, wt, dt if ycode is None else int(ycode),
           LA_E4M3 if kcode is None else int(kcode))
 
 
@@ -755,8 +759,8 @@ def la_rmsnorm_backward(total, scales, weight, rstd, dy, dtotal, dx, dweight, wo
         raise ValueError("dweight must be float32, of the weight's shape")
     _per_row(dy, rstd=rstd)
     rows, C = _rows(dy)
-    _call("la_rmsnorm_backward", dy, stream, _ptr(total), _ptr(scales), _ptr(weight), _ptr(rstd), _ptr(dy), _ptr(dtotal),
-          _ptr(dx), _ptr(dweight), rows, C, dt, wt, dt if code is None else int(code), *_room(workspace))
+    _call("la_rmsnorm_backward", dy, stream, (dx, dweight), _ptr(total), _ptr(scales), _ptr(weight), _ptr(rstd), _ptr(dy),
+          _ptr(dtotal), _ptr(dx), _ptr(dweight), rows, C, dt, wt, dt if code is None else int(code), *_room(workspace))
 
 
 def in_native_code(name, where, *args):

@@ -224,7 +224,11 @@ PyObject *recurrence_step(PyObject *, PyObject *const *a, Py_ssize_t n)
         const la_gate gate = (la_gate)PyLong_AsLong(a[4]);
         void *const st = stream_of(a[5], x), *const p[] = {address(a[0]), address(a[1]), address(a[2]), address(a[3])};
         const c10::DeviceGuard guard(x.device());
-        return status([&] { return rec_step(p[0], p[1], p[2], (float *)p[3], s.B, s.N, s.C, gate, s.dt, st); });
+        PyObject *const rc = status([&] { return rec_step(p[0], p[1], p[2], (float *)p[3], s.B, s.N, s.C, gate, s.dt, st); });
+        if (rc && PyLong_AsLong(rc) == 0)  // a node that saved what was written must not go on with the new values
+            for (int i : {2, 3})
+                if (!tensor(a[i]).is_inference()) tensor(a[i]).unsafeGetTensorImpl()->bump_version();
+        return rc;
     });
 }
 
