@@ -17,8 +17,9 @@ Every call can be captured into a graph, a training step too: run it a few times
 let go of the results (no eager graph of the same leaves may be alive while a backward pass is captured: torch
 then joins streams inside the capture), and take the gradients from torch.autograd.grad.
 """
+import functools
+
 import torch
-from torch.autograd.function import once_differentiable
 
 from . import binding as _b
 
@@ -29,6 +30,25 @@ def _code(t):
 
 def _bytes(n, device):
     return torch.empty(max(int(n), 256), dtype=torch.uint8, device=device)
+
+
+def _once(backward):
+    """Gradients of gradients are not defined: where a graph of the backward pass is asked for, its results come out
+    of a node that refuses, tied to the incoming gradients and the tensors that were kept."""
+    @functools.wraps(backward)
+    def refusing(ctx, *grads):
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        if not torch.is_grad_enabled():
+            return out
+        ends = [t.detach().requires_grad_(True) for t in out if t is not None]
+        ties = [t for t in (*ctx.saved_tensors, *grads) if t is not None and t.requires_grad]
+        refuse = torch._C._functions.DelayedError(b"gradients of gradients are not defined for this operator",
+                                                  len(ends) + len(ties))
+        ends = refuse(*ends, *ties)
+        ends = iter((ends,) if isinstance(ends, torch.Tensor) else ends)
+        return tuple(None if t is None else next(ends) for t in out)
+    return refusing
 
 
 class LinearAttentionFunction(torch.autograd.Function):
@@ -85,7 +105,7 @@ class CheckpointedAttentionFunction(torch.autograd.Function):
         return O
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, dO):
         return (*checkpointed_backward(*ctx.saved_tensors, dO.contiguous(), *ctx.la_args), None, None, None, None, None)
 
@@ -171,7 +191,7 @@ class GatedRecurrenceFunction(torch.autograd.Function):
         return h, last
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, dh, dlast):
         x = ctx.saved_tensors[0]
         dh = torch.zeros_like(x) if dh is None else dh.contiguous()
@@ -228,7 +248,7 @@ class RmsNormFunction(torch.autograd.Function):
         return y, total
 
     @staticmethod
-    @once_differentiable
+    @_once
     def backward(ctx, dy, dtotal):
         if dy is None:  # the sum alone was used
             return dtotal, dtotal if ctx.needs_input_grad[1] else None, None, None, None

@@ -5,6 +5,7 @@
 // D = 16, 235 and 91; rms_norm_quantised on 8 rows 17 and 7.0; a step of a recurrence 8.3 and 4.0.
 #include <c10/core/DeviceGuard.h>
 #include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
 
 #include "la_bind.h"
 
@@ -44,20 +45,19 @@ bool fits(const at::Tensor &t, const at::Tensor &ref, at::ScalarType type, at::I
                             t.get_device() == ref.get_device() && t.scalar_type() == type && t.sizes() == sizes);
 }
 
-// Gradients of gradients are not defined: where a graph of the backward pass is asked for, its results end in an error.
+// Gradients of gradients are not defined: where a graph of the backward pass is asked for, its results come out of a node
+// that refuses, tied to all that they depend on (the operator's inputs and the incoming gradients), so that no
+// derivative goes past it.
 variable_list once(variable_list out, const variable_list &grads)
 {
-    bool asked = false;
-    for (const at::Tensor &g : grads) asked |= g.defined() && g.requires_grad();
-    if (!asked || !at::GradMode::is_enabled()) return out;
+    using namespace torch::autograd;
+    if (!at::GradMode::is_enabled()) return out;
+    edge_list edges = collect_next_edges(grads);
+    if (const auto node = get_current_node()) edges.insert(edges.end(), node->next_edges().begin(), node->next_edges().end());
+    const auto refuse =
+        std::make_shared<Error>("gradients of gradients are not defined for this operator", std::move(edges));
     for (at::Tensor &t : out)
-        if (t.defined()) {
-            auto node = std::make_shared<torch::autograd::DelayedError>(
-                "gradients of gradients are not defined for this operator", 1);
-            t = t.detach();
-            t.set_requires_grad(true);
-            t = (*node)({t})[0];
-        }
+        if (t.defined()) set_history(t = t.detach(), refuse);
     return out;
 }
 
@@ -178,7 +178,7 @@ struct Recurrence : torch::autograd::Function<Recurrence> {
                                                                          wrapped(h), wrapped(lengths), wrapped(dh),
                                                                          wrapped(dlast), (long long)gate, (int)wants_h0));
         out.resize(5);
-        return out;
+        return once(std::move(out), grads);
     }
 };
 
@@ -346,7 +346,7 @@ struct RmsNorm : torch::autograd::Function<RmsNorm> {
                                                      wrapped(rstd), wrapped(dy), wrapped(dtotal), (long long)code,
                                                      (int)wants_res, (int)wants_w));
         out.resize(5);
-        return out;
+        return once(std::move(out), grads);
     }
 };
 
@@ -482,7 +482,7 @@ struct Checkpointed : torch::autograd::Function<Checkpointed> {
                           Py_BuildValue("NNNddiiLi", wrapped(codes), wrapped(powers), wrapped(dO), a, b, (int)causal, (int)norm,
                                         (long long)code, (int)(dt == LA_F32)));
         out.resize(8);
-        return out;
+        return once(std::move(out), grads);
     }
 };
 
