@@ -308,16 +308,21 @@ struct Shape {
     int lanes() const { return L ? Share<L>::NT : (C + 512 * K - 1) / (512 * K) * 64; }  // of a workgroup
     int rows() const { return Share<L>::ROWS; }
 };
-template <typename F>
-void by_width(int C, bool backward, F f)
+template <bool BACKWARD, typename F>
+void by_width(int C, F f)
 {
     if (C <= 64) f(Shape<8, 1>{C});
     else if (C <= 128) f(Shape<16, 1>{C});
     else if (C <= 256) f(Shape<32, 1>{C});
     else if (C <= 512) f(Shape<64, 1>{C});
-    else if (C <= 1024) backward ? f(Shape<128, 1>{C}) : f(Shape<64, 2>{C});
-    else if (backward && C <= 8192) f(Shape<0, 1>{C});
-    else f(Shape<0, 2>{C});
+    else if constexpr (BACKWARD) {
+        if (C <= 1024) f(Shape<128, 1>{C});
+        else if (C <= 8192) f(Shape<0, 1>{C});
+        else f(Shape<0, 2>{C});
+    } else {
+        if (C <= 1024) f(Shape<64, 2>{C});
+        else f(Shape<0, 2>{C});
+    }
 }
 // Workgroups that take all rows in one go.
 template <typename S>
@@ -331,7 +336,7 @@ size_t row_groups(size_t rows, S shape)
 int back_blocks(size_t rows, int C)
 {
     int n = 0;
-    by_width(C, true, [&](auto shape) {
+    by_width<true>(C, [&](auto shape) {
         const size_t g = row_groups(rows, shape), most = 256 * (4 / ((shape.lanes() / 64 + 3) / 4));
         const size_t few = g / 4 > 256 ? g / 4 : 256;
         n = (int)(g < few ? g : few < most ? few : most);
@@ -447,7 +452,7 @@ la_status la_rmsnorm_forward(const void *X, const void *R, const void *W, void *
     if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
     const la::Norm a{X, R, W, Y, S, (uint8_t *)Yscale, (uint8_t *)Kept, (uint8_t *)Kscale, rstd, rows, C, eps, yt, kt};
     la::by_types(dt, wt, [&](auto *t, auto *w) {
-        la::by_width(C, false, [&](auto shape) {
+        la::by_width<false>(C, [&](auto shape) {
             typedef decltype(shape) Sh;
             const size_t groups = la::row_groups(rows, shape);
             const dim3 grid((unsigned)(groups < 65536 ? groups : 65536));
@@ -482,7 +487,7 @@ la_status la_rmsnorm_backward(const void *S, const void *Sscale, const void *W, 
     const int blocks = la::back_blocks(rows, C);
     const hipStream_t stream = (hipStream_t)hip_stream;
     la::by_types(dt, wt, [&](auto *t, auto *w) {
-        la::by_width(C, true, [&](auto shape) {
+        la::by_width<true>(C, [&](auto shape) {
             typedef decltype(shape) Sh;
             la::k_norm_back<std::remove_pointer_t<decltype(t)>, std::remove_pointer_t<decltype(w)>, Sh::l, Sh::k>
                 <<<dim3(blocks), dim3(shape.lanes()), 0, stream>>>(a);
