@@ -392,8 +392,8 @@ LA_API la_status la_backward_traced(const void *Q, const void *K, const void *V,
                       la_trace *trace);
 
 /*
- * Gated linear recurrence: the recurrence of App. B.1 with a gate per row and channel (the form that
- * Table 3's gated rows share), on a vector state.  For each of B sequences of N rows with C channels
+ * Gated linear recurrence: the recurrence of App. B.1 with a gate per row and channel, on a vector state (not
+ * the matrix states of the gated rows of Table 3).  For each of B sequences of N rows with C channels
  *
  *     h_t = f_t h_{t-1} + u_t          (element-wise, t = 0 .. N-1, h_{-1} = h0)
  *     LA_GATE_VALUE:    f_t = g_t,             u_t = x_t
@@ -422,7 +422,8 @@ LA_API la_status la_backward_traced(const void *Q, const void *K, const void *V,
  * of a run of gates has to be a float (gates of magnitude up to 1 are); an infinity or a NaN spoils its
  * channel from its row on (backward: up to it), whatever the gates after it.
  * Calls that share a workspace must not overlap in time, two captured graphs' neither: workgroups of one
- * call wait for words that others of it leave there.  (Such waits are bounded: the results are then NaN.)
+ * call wait for words that others of it leave there.  Results of calls that overlap all the same are undefined: wrong
+ * finite values, rows left unwritten or NaN, with LA_OK; the waits are bounded only so that the kernels end.
  * Limits: B, N, C >= 1, N <= 2^30, B*N*C < 2^40, B * ceil(C / 64) < 2^23 and, times ceil(N / 64), < 2^31.
  *
  * la_recurrence_step appends T rows to a carried state, [B, C] float32, and updates it in place: the

@@ -126,7 +126,8 @@ __device__ __forceinline__ uint64_t peek(const uint64_t *p)
 }
 // A word that was peeked at, once it is there.  Within one call every wait ends (above) in microseconds; where two calls
 // overlap on one workspace, against the rules, one may wipe out what the other waits for: after some seconds of looking
-// a wait ends with what is there, ones, which are NaN in either half and spoil the results.
+// a wait ends with what is there, ones, which are NaN in either half.  That ends the kernel and tells nothing: such calls
+// may as well take each other's finite words, or leave out the tiles whose tickets the other drew.
 __device__ __forceinline__ uint64_t await(const uint64_t *p, uint64_t word)
 {
     for (int looks = 0; (uint32_t)(word >> 32) == kNothing && looks < kMostLooks; ++looks) {
