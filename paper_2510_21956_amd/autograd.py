@@ -166,7 +166,7 @@ def unpack_rows(codes, scales, code, dtype):
 def _eight_bits(x, code, *count):
     """Room for x's codes and powers (for `count` tensors like x)."""
     kind = torch.float8_e4m3fn if code == _b.LA_E4M3 else torch.int8
-    groups = (*count, *x.shape[:-1], -(-x.shape[-1] // _b.LA_GROUP))
+    groups = (*count, *_b.powers_shape(x.shape))
     return (torch.empty((*count, *x.shape), dtype=kind, device=x.device),
             torch.empty(groups, dtype=torch.float8_e8m0fnu, device=x.device))
 

@@ -637,6 +637,13 @@ def eight_bit_code(name):
     return _EIGHT[name]
 
 
+def powers_shape(shape):
+    """The shape of the powers of rows of ``shape``, one for every 32 elements."""
+    if len(shape) < 1:
+        raise ValueError("rows of [..., C] are needed")
+    return (*shape[:-1], -(-shape[-1] // LA_GROUP))
+
+
 def _eight(codes, scales, x, code, what):
     """Checks codes like x and a power for every 32 elements of a row; both of one byte an element."""
     if code not in (LA_E4M3, LA_I8):
@@ -644,9 +651,9 @@ def _eight(codes, scales, x, code, what):
     _needed(**{what + " codes": codes, what + " scales": scales})
     if codes.shape != x.shape or codes.element_size() != 1:
         raise ValueError("%s codes must be %s of one byte an element" % (what, tuple(x.shape)))
-    groups = x.shape[:-1] + (-(-x.shape[-1] // LA_GROUP),)
+    groups = powers_shape(x.shape)
     if scales.shape != groups or scales.element_size() != 1:
-        raise ValueError("%s scales must be %s of one byte an element" % (what, tuple(groups)))
+        raise ValueError("%s scales must be %s of one byte an element" % (what, groups))
 
 
 def _rows(x):
