@@ -24,7 +24,7 @@ typedef uint32_t words4 __attribute__((ext_vector_type(4), aligned(2)));  // at 
 // A lane's place in a row of C elements: eight from element c on, `valid` of them in the row (none where the row is not
 // `here`).  Eight elements of the row are loaded in one go whatever the place, the row's last ones from its end on, and
 // moved down by `shift` once they are there: loads that only some lanes make, or of single elements, cost branches
-// and waits for every row (30000 rows of 771, bf16, backward 49 us; with both 83).
+// and waits for every row (30000 rows of 771, bf16, backward 45 us; with both 83).
 struct Span {
     int c, valid, shift;
     __device__ __forceinline__ Span(int c, int C, bool here = true)

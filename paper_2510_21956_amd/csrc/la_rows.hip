@@ -331,8 +331,9 @@ size_t row_groups(size_t rows, S shape)
     return (rows + shape.rows() - 1) / shape.rows();
 }
 // Workgroups of the backward pass: as many as run at once (four waves of its registers to a SIMD, whose share of a
-// workgroup's waves is rounded up), each with a share of dw, and fewer where each would get less than four rows to
-// itself: 16384 rows of 2056, bf16, 512 workgroups 61 us, 1024 87; 1000 of 2048, 250 workgroups 11.0, 1000 16.3.
+// workgroup's waves is rounded up), each with a share of dw, and fewer, down to one for each of the 256 compute units, where
+// each would get less than four rows to itself: 16384 rows of 2056, bf16, 512 workgroups 61 us, 1024 87; 1000 of 2048, 256
+// workgroups 11.0, 1000 16.3.
 int back_blocks(size_t rows, int C)
 {
     int n = 0;
