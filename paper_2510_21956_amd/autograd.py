@@ -33,16 +33,23 @@ def _bytes(n, device):
 
 
 def _once(backward):
-    """Gradients of gradients are not defined: where a graph of the backward pass is asked for, its results come out
-    of a node that refuses, tied to the incoming gradients and the tensors that were kept."""
+    """``backward`` gets the saved tensors as a call that unpacks them one time, whatever hooks they went through.
+    Gradients of gradients are not defined: where a graph of the backward pass is asked for, results that depend on them
+    come out of a node that refuses, tied to the incoming gradients and the tensors that were kept."""
     @functools.wraps(backward)
     def refusing(ctx, *grads):
+        kept = []
+
+        def saved():
+            if not kept:
+                kept.append(ctx.saved_tensors)
+            return kept[0]
         with torch.no_grad():
-            out = backward(ctx, *grads)
-        if not torch.is_grad_enabled():
+            out = backward(ctx, saved, *grads)
+        if not kept or not torch.is_grad_enabled():
             return out
         ends = [t.detach().requires_grad_(True) for t in out if t is not None]
-        ties = [t for t in (*ctx.saved_tensors, *grads) if t is not None and t.requires_grad]
+        ties = [t for t in (*kept[0], *grads) if t is not None and t.requires_grad]
         refuse = torch._C._functions.DelayedError(b"gradients of gradients are not defined for this operator",
                                                   len(ends) + len(ties))
         ends = refuse(*ends, *ties)
@@ -106,8 +113,8 @@ class CheckpointedAttentionFunction(torch.autograd.Function):
 
     @staticmethod
     @_once
-    def backward(ctx, dO):
-        return (*checkpointed_backward(*ctx.saved_tensors, dO.contiguous(), *ctx.la_args), None, None, None, None, None)
+    def backward(ctx, saved, dO):
+        return (*checkpointed_backward(*saved(), dO.contiguous(), *ctx.la_args), None, None, None, None, None)
 
 
 def checkpointed_backward(codes, scales, dO, a, b, causal, normalize_qk, code, single):
@@ -192,11 +199,11 @@ class GatedRecurrenceFunction(torch.autograd.Function):
 
     @staticmethod
     @_once
-    def backward(ctx, dh, dlast):
-        x = ctx.saved_tensors[0]
+    def backward(ctx, saved, dh, dlast):
+        x = saved()[0]
         dh = torch.zeros_like(x) if dh is None else dh.contiguous()
         dlast = dlast if dlast is None else dlast.contiguous()
-        return (*recurrence_backward(*ctx.saved_tensors, dh, dlast, ctx.la_gate, ctx.needs_input_grad[2]), None, None)
+        return (*recurrence_backward(*saved(), dh, dlast, ctx.la_gate, ctx.needs_input_grad[2]), None, None)
 
 
 def recurrence_backward(x, gates, h0, h, lengths, dh, dlast, gate, wants_h0):
@@ -249,11 +256,11 @@ class RmsNormFunction(torch.autograd.Function):
 
     @staticmethod
     @_once
-    def backward(ctx, dy, dtotal):
+    def backward(ctx, saved, dy, dtotal):
         if dy is None:  # the sum alone was used
             return dtotal, dtotal if ctx.needs_input_grad[1] else None, None, None, None
         dtotal = dtotal if dtotal is None else dtotal.contiguous()
-        return (*norm_backward(*ctx.saved_tensors, dy.contiguous(), dtotal, -1 if ctx.la_code is None else ctx.la_code,
+        return (*norm_backward(*saved(), dy.contiguous(), dtotal, -1 if ctx.la_code is None else ctx.la_code,
                                ctx.needs_input_grad[1], ctx.needs_input_grad[2]), None, None)
 
 
