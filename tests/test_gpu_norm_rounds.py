@@ -83,3 +83,32 @@ def test_every_row_counts_once_in_dw(rows, C, dtype):
         saved, powers = (s, None) if code is None else la.pack_rows(s, code)
         la.la_rmsnorm_backward(saved, powers, w, rstd, dy, None, dx, dw, ws, CODE[code] if code else None)
         assert torch.equal(dw.double(), want), code
+
+
+@pytest.mark.parametrize("code", [None, "int8"])
+def test_offsets_beyond_32_bits(code):
+    """More than 2^31 elements and 2^32 bytes: the last rows' gradients, and dw, which they alone make."""
+    rows, C, last = 140000, 16384, 3
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    s, dy = (torch.zeros((rows, C), device="cuda", dtype=torch.bfloat16) for _ in range(2))
+    s[-last:] = torch.randn((last, C), device="cuda", generator=gen).to(torch.bfloat16)
+    dy[-last:] = torch.randn((last, C), device="cuda", generator=gen).to(torch.bfloat16)
+    w = 1 + 0.1 * torch.randn(C, device="cuda", generator=gen)
+    _, inv = norm64(s[-last:], w, EPS)
+    rstd = torch.ones(rows, device="cuda")
+    rstd[-last:] = inv[:, 0].float()
+    saved, powers = (s, None) if code is None else la.pack_rows(s, code)
+    if code:
+        back = la.unpack_rows(saved, powers, code, torch.bfloat16)
+        assert torch.equal(back[-last:], la.unpack_rows(saved[-last:], powers[-last:], code, torch.bfloat16))
+        assert not back[:-last].any()
+        del back
+    dx, dw = torch.full_like(s, float("nan")), torch.empty(C, device="cuda")
+    ws = torch.empty(la.la_rmsnorm_workspace_bytes(rows, C), dtype=torch.uint8, device="cuda")
+    la.la_rmsnorm_backward(saved, powers, w, rstd, dy, None, dx, dw, ws, CODE[code] if code else None)
+    at = s[-last:] if code is None else la.unpack_rows(saved[-last:], powers[-last:], code, torch.float32)
+    wx, ww, Ex, Ew = norm_backward64(at, inv, w, dy[-last:], None)
+    close(dx[-last:], wx, Ex, torch.bfloat16)
+    assert not dx[:-last].any()
+    # the rows of zeros add nothing: the bound is that of the three
+    close(dw, ww, Ew, torch.float32)
