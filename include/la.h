@@ -516,6 +516,113 @@ LA_API la_status la_rmsnorm_backward(const void *S, const void *Sscale, const vo
                       size_t rows, int C, la_dtype dt, la_dtype wt, la_dtype st,
                       void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/*
+ * Short causal convolution along the rows, one filter of W taps a channel, with an activation: what stands in front of
+ * a selective scan.  For each of B sequences of N rows with C channels
+ *
+ *     v_t = bias + sum_{j < W} w_j x_{t-(W-1)+j},   y_t = v_t (LA_ACT_NONE) or v_t / (1 + exp(-v_t)) (LA_ACT_SILU)
+ *
+ * where the W - 1 rows before the first are `state`, the rows carried from an earlier call, or zeros; and backward,
+ * with e_t = dy_t dy/dv (zero outside of the sequence),
+ *
+ *     dx_t = sum_j w_j e_{t+(W-1)-j},   dw_j = sum_t e_t x_{t-(W-1)+j},   dbias = sum_t e_t   (over the sequences too)
+ *
+ *   X: B * N rows of C elements of `dt` (LA_F32 / LA_BF16), x_stride >= C elements from one row to the next: a part of wider
+ *       rows may be given as it is.  Y, dY, dX: [B, N, C] of `dt`, dense.
+ *   Wt: [C, W]; bias: [C], or NULL for zeros; both of `wt`, LA_F32 or `dt`.  2 <= W <= 8.
+ *   state: [B, W - 1, C] of `dt`, oldest row first, NULL: zeros.  last: the W - 1 rows to carry on, NULL: not wanted; where a
+ *       sequence has fewer rows than that, those of `state` move up.  last must not be state itself.
+ *   dlast, dstate: their gradients, [B, W - 1, C] of `dt`; dlast NULL: zeros, dstate NULL: not wanted.
+ *   dW: [C, W] float32, dbias: [C] float32, or NULL where they are not wanted.
+ *   lengths: NULL, or B ints on the device.  Rows from lengths[b] on are padding: they are not read, every output is zero there
+ *       (a length of 0 or less: `last` is `state`; one of N or more is N).
+ *   workspace (only where dW or dbias is wanted): at least la_conv_workspace_bytes(B, N, C, W) bytes, 256-byte aligned.
+ * Sums are float32, those of dW and dbias in a fixed order.  Addresses are those of elements.
+ * Limits: B, N, C >= 1, N <= 2^30, B * N * x_stride < 2^40, B * C * ceil(N / 16) < 2^31.
+ *
+ * la_conv_step appends T rows to the carried ones, which it updates in place: the form for single tokens.  Rows are walked one
+ * after another, T is meant to be small.  Calls that share a state must not overlap in time.
+ * Error behaviour as for la_forward; an unknown activation is LA_ERR_UNSUPPORTED.
+ */
+typedef enum la_act {
+    LA_ACT_NONE = 0,
+    LA_ACT_SILU = 1
+} la_act;
+
+LA_API size_t la_conv_workspace_bytes(int B, int N, int C, int W);
+
+LA_API la_status la_conv_forward(const void *X, size_t x_stride, const void *Wt, const void *bias, const void *state,
+                     void *Y, void *last, const int *lengths,
+                     int B, int N, int C, int W, la_act act, la_dtype dt, la_dtype wt, void *hip_stream);
+
+LA_API la_status la_conv_backward(const void *X, size_t x_stride, const void *Wt, const void *bias, const void *state,
+                     const void *dY, const void *dlast, void *dX, float *dW, float *dbias, void *dstate,
+                     const int *lengths, int B, int N, int C, int W, la_act act, la_dtype dt, la_dtype wt,
+                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+LA_API la_status la_conv_step(const void *X, size_t x_stride, const void *Wt, const void *bias, void *state, void *Y,
+                     int B, int T, int C, int W, la_act act, la_dtype dt, la_dtype wt, void *hip_stream);
+
+/*
+ * Selective state space scan: a recurrence with S states to a channel, whose decays and inputs depend on the row, read out by a
+ * vector that does too.  For each of B sequences of N rows with C channels c, in G groups of C / G neighbours that share
+ * B_t and C_t, and states s < S
+ *
+ *     d_t[c] = softplus(dt_t[c] + bias[c]) (LA_STEP_SOFTPLUS: log(1 + exp(.))) or dt_t[c] + bias[c] (LA_STEP_VALUE)
+ *     h_t[c,s] = exp(d_t[c] A[c,s]) h_{t-1}[c,s] + d_t[c] x_t[c] B_t[s],     y_t[c] = sum_s C_t[s] h_t[c,s] + D[c] x_t[c]
+ *
+ * and backward, with g_t = C_t dy_t + exp(d_{t+1} A) g_{t+1} (from dlast behind the last row) and e_t = g_t exp(d_t A) h_{t-1},
+ *
+ *     dx_t = d_t sum_s g_t B_t + D dy_t,     dd_t = x_t sum_s g_t B_t + sum_s e_t A,     ddt_t = dd_t or dd_t / (1 + exp(-dt_t - bias))
+ *     dB_t = sum_c g_t d_t x_t,   dC_t = sum_c dy_t h_t   (over the channels of the group),   dh0 = exp(d_0 A) g_0
+ *     dA = sum_t e_t d_t,   dD = sum_t dy_t x_t,   dbias = sum_t ddt_t   (over the sequences too)
+ *
+ *   X, Dt: B * N rows of C elements of `dt` (LA_F32 / LA_BF16), Bm, Cm: B * N rows of G * S; x_stride, dt_stride, b_stride,
+ *       c_stride elements from one row to the next: parts of wider rows may be given as they are.
+ *       Y, dY, dX, dDt: [B, N, C], dBm, dCm: [B, N, G, S] of `dt`, dense.
+ *   A: [C, S] float32 (the decays exp(d A) have to be floats, and so has their product over a run of rows: A < 0 with d >= 0).
+ *       D, bias: [C] float32, or NULL for zeros.  dA, dD, dbias: their gradients, float32, or NULL where they are not wanted.
+ *   h0, last, dlast, dh0: [B, C, S] float32.  h0 NULL: zeros; last (the state after the last row) NULL: not wanted; dlast NULL:
+ *       zeros; dh0 NULL: not wanted.
+ *   saved: states that the forward call leaves for the backward call, la_selective_saved_bytes(B, N, C, S) bytes, 256-byte aligned;
+ *       NULL in a forward call that no backward call follows.  Its layout is private to the library.
+ *   lengths: NULL, or B ints on the device.  Rows from lengths[b] on are padding: they are not read, every output is zero there, and
+ *       `last` is the state before them (a length of 0 or less leaves h0, one of N or more is N).
+ *   workspace: at least la_selective_workspace_bytes(B, N, C, S, G, is_backward) bytes, 256-byte aligned; NULL where that is 0.
+ *       Nothing in it has to start at zero.  Calls that share one must not overlap in time, two captured graphs' neither.
+ * States, products and sums are float32, the sums in a fixed order: two runs give the same bits.  Addresses are those of elements.
+ * Limits: B, N, C, S, G >= 1, N <= 2^30, S <= 128, C a multiple of G, B * N * stride < 2^40 for every tensor,
+ * B * G * ceil(C / G / 64) * ceil(N / 16) < 2^31 and, without the last factor, < 2^21.
+ *
+ * la_selective_step appends T rows to a carried state, [B, C, S] float32, and updates it in place: the form for single
+ * tokens.  No workspace; rows are walked one after another, T is meant to be small.  Calls that share a state must not overlap in time.
+ * Error behaviour as for la_forward; an unknown step is LA_ERR_UNSUPPORTED.
+ */
+typedef enum la_step {
+    LA_STEP_VALUE = 0,
+    LA_STEP_SOFTPLUS = 1
+} la_step;
+
+LA_API size_t la_selective_workspace_bytes(int B, int N, int C, int S, int G, int is_backward);
+LA_API size_t la_selective_saved_bytes(int B, int N, int C, int S);
+
+LA_API la_status la_selective_forward(const void *X, size_t x_stride, const void *Dt, size_t dt_stride, const float *A,
+                     const void *Bm, size_t b_stride, const void *Cm, size_t c_stride, const float *D, const float *bias,
+                     const float *h0, void *Y, float *last, void *saved, size_t saved_bytes, const int *lengths,
+                     int B, int N, int C, int S, int G, la_step step, la_dtype dt,
+                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+LA_API la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, size_t dt_stride, const float *A,
+                     const void *Bm, size_t b_stride, const void *Cm, size_t c_stride, const float *D, const float *bias,
+                     const void *saved, size_t saved_bytes, const void *dY, const float *dlast,
+                     void *dX, void *dDt, float *dA, void *dBm, void *dCm, float *dD, float *dbias, float *dh0,
+                     const int *lengths, int B, int N, int C, int S, int G, la_step step, la_dtype dt,
+                     void *workspace, size_t workspace_bytes, void *hip_stream);
+
+LA_API la_status la_selective_step(const void *X, size_t x_stride, const void *Dt, size_t dt_stride, const float *A,
+                     const void *Bm, size_t b_stride, const void *Cm, size_t c_stride, const float *D, const float *bias,
+                     float *state, void *Y, int B, int T, int C, int S, int G, la_step step, la_dtype dt, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

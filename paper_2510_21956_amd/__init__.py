@@ -13,9 +13,12 @@ from .binding import (EXPORTS, LA_BF16, LA_F32, LA_MAX_TRACE, LaError, la_backwa
 from .binding import (LA_E4M3, LA_GATE_SIGMOID, LA_GATE_VALUE, LA_GROUP, LA_I8, la_pack_rows, la_pack_tensors, la_recurrence_backward,
                       la_recurrence_forward, la_recurrence_step, la_recurrence_workspace_bytes, la_rmsnorm_backward,
                       la_rmsnorm_forward, la_rmsnorm_workspace_bytes, la_unpack_rows)
+from .binding import (LA_ACT_NONE, LA_ACT_SILU, LA_STEP_SOFTPLUS, LA_STEP_VALUE, la_conv_backward, la_conv_forward, la_conv_step,
+                      la_conv_workspace_bytes, la_selective_backward, la_selective_forward, la_selective_saved_bytes,
+                      la_selective_step, la_selective_workspace_bytes)
 
-from .autograd import (LinearAttentionFunction, gated_recurrence, linear_attention, pack_rows, rms_norm,
-                       rms_norm_quantised, unpack_rows)
+from .autograd import (LinearAttentionFunction, causal_conv, gated_recurrence, linear_attention, pack_rows, rms_norm,
+                       rms_norm_quantised, selective_scan, unpack_rows)
 
 __all__ = ["LinearAttentionFunction", "linear_attention", "LA_F32", "LA_BF16", "LA_MAX_TRACE", "EXPORTS", "LaError", "la_forward", "la_backward",
            "la_forward_traced", "la_backward_traced", "la_forward_save", "la_backward_saved",
@@ -24,4 +27,7 @@ __all__ = ["LinearAttentionFunction", "linear_attention", "LA_F32", "LA_BF16", "
            "gated_recurrence", "rms_norm", "rms_norm_quantised", "pack_rows", "unpack_rows", "LA_E4M3", "LA_I8",
            "LA_GROUP", "LA_GATE_VALUE", "LA_GATE_SIGMOID", "la_recurrence_workspace_bytes", "la_recurrence_forward",
            "la_recurrence_backward", "la_recurrence_step", "la_pack_rows", "la_pack_tensors", "la_unpack_rows",
-           "la_rmsnorm_workspace_bytes", "la_rmsnorm_forward", "la_rmsnorm_backward"]
+           "la_rmsnorm_workspace_bytes", "la_rmsnorm_forward", "la_rmsnorm_backward",
+           "causal_conv", "selective_scan", "LA_ACT_NONE", "LA_ACT_SILU", "LA_STEP_VALUE", "LA_STEP_SOFTPLUS",
+           "la_conv_workspace_bytes", "la_conv_forward", "la_conv_backward", "la_conv_step", "la_selective_workspace_bytes",
+           "la_selective_saved_bytes", "la_selective_forward", "la_selective_backward", "la_selective_step"]

@@ -302,3 +302,133 @@ def rms_norm_quantised(x, weight=None, residual=None, eps=1e-6, code="e4m3"):
     total = None if residual is None else torch.empty_like(x)
     _b.la_rmsnorm_forward(x, residual, weight, codes, scales, total, None, None, None, eps, code)
     return (codes, scales) if residual is None else (codes, scales, total)
+
+
+# ---- the selective state space layer ----------------------------------------------------------
+
+def _rows_in_place(t, dims=1):
+    """t as the kernels take it: rows that are dense and at one distance, else a copy."""
+    return t if t is None or _b.row_stride(t, dims) is not None else t.contiguous()
+
+
+def _dense(t):
+    return t if t is None else t.contiguous()
+
+
+class CausalConvFunction(torch.autograd.Function):
+    """y_t = act(bias + sum_j w_j x_{t-(W-1)+j}) (la_conv_forward); x: [..., N, C] device tensors."""
+
+    @staticmethod
+    def forward(ctx, x, weight, bias, state, lengths, act):
+        x, weight, bias, state, lengths = _rows_in_place(x), *map(_dense, (weight, bias, state, lengths))
+        if x.dim() < 2 or weight.dim() != 2:
+            raise ValueError("x must be [..., N, C] and the weight [C, taps]")
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        last = torch.empty((*x.shape[:-2], weight.shape[1] - 1, x.shape[-1]), dtype=x.dtype, device=x.device)
+        _b.la_conv_forward(x, weight, bias, state, y, last, lengths, act)
+        ctx.save_for_backward(x, weight, bias, state, lengths)
+        ctx.la_act = act
+        ctx.set_materialize_grads(False)
+        return y, last
+
+    @staticmethod
+    @_once
+    def backward(ctx, saved, dy, dlast):
+        x = saved()[0]
+        dy = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if dy is None else dy.contiguous()
+        return (*conv_backward(*saved(), dy, _dense(dlast), ctx.la_act, *ctx.needs_input_grad[1:4]), None, None)
+
+
+def conv_backward(x, weight, bias, state, lengths, dy, dlast, act, wants_weight, wants_bias, wants_state):
+    dx = torch.empty_like(dy)
+    dw = torch.empty(weight.shape, dtype=torch.float32, device=x.device) if wants_weight else None
+    db = torch.empty(weight.shape[:1], dtype=torch.float32, device=x.device) if wants_bias else None
+    ds = torch.empty_like(state) if wants_state else None
+    ws = None
+    if wants_weight or wants_bias:
+        N, C = x.shape[-2:]
+        ws = _bytes(_b.la_conv_workspace_bytes(x.numel() // (N * C) if x.numel() else 0, N, C, weight.shape[1]), x.device)
+    _b.la_conv_backward(x, weight, bias, state, dy, dlast, dx, dw, db, ds, lengths, act, ws)
+    return dx, dw if dw is None else dw.to(weight.dtype), db if db is None else db.to(bias.dtype), ds
+
+
+_ACTS = {"none": _b.LA_ACT_NONE, "silu": _b.LA_ACT_SILU}
+_STEPS = {"value": _b.LA_STEP_VALUE, "softplus": _b.LA_STEP_SOFTPLUS}
+
+
+def causal_conv(x, weight, bias=None, state=None, lengths=None, activation="silu"):
+    """Differentiable causal convolution along the second to last dimension of x [..., N, C] (float32 or bfloat16 device
+    tensors; a part of wider rows is read where it is), one filter of 2 to 8 taps a channel:
+    y_t = act(bias + sum_j weight[:, j] x_{t-(W-1)+j}), activation "silu" or "none"; weight [C, W] and bias [C] float32 or x's type.
+
+    state [..., W - 1, C] like x: the rows before the first (None: zeros).  lengths [...] int32: rows from there on are
+    padding, zero in every output.  Returns y like x and the last W - 1 rows of every sequence, from which la_conv_step and another
+    call's state go on."""
+    if activation not in _ACTS:
+        raise ValueError("activations are %s, got %r" % (" and ".join(map(repr, _ACTS)), activation))
+    return CausalConvFunction.apply(x, weight, bias, state, lengths, _ACTS[activation])
+
+
+class SelectiveScanFunction(torch.autograd.Function):
+    """h_t = exp(d_t A) h_{t-1} + d_t x_t B_t, y_t = C_t h_t + D x_t (la_selective_forward); x: [..., N, C] device tensors."""
+
+    @staticmethod
+    def forward(ctx, x, dt, A, B, C, D, bias, h0, lengths, step, keeps):
+        dims = 1 if B.dim() == x.dim() else 2
+        x, dt, B, C = _rows_in_place(x), _rows_in_place(dt), _rows_in_place(B, dims), _rows_in_place(C, dims)
+        A, D, bias, h0, lengths = map(_dense, (A, D, bias, h0, lengths))
+        sizes = _scan_sizes(x, A, B)
+        y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        last = torch.empty((*x.shape[:-2], *A.shape), dtype=torch.float32, device=x.device)
+        saved = _bytes(_b.la_selective_saved_bytes(*sizes[:4]), x.device) if keeps else None
+        n = _b.la_selective_workspace_bytes(*sizes, 0)
+        _b.la_selective_forward(x, dt, A, B, C, D, bias, h0, y, last, saved, lengths, step, _bytes(n, x.device) if n else None)
+        ctx.save_for_backward(x, dt, A, B, C, D, bias, lengths, saved)
+        ctx.la_step = step
+        ctx.set_materialize_grads(False)
+        return y, last
+
+    @staticmethod
+    @_once
+    def backward(ctx, saved, dy, dlast):
+        x = saved()[0]
+        dy = torch.zeros(x.shape, dtype=x.dtype, device=x.device) if dy is None else dy.contiguous()
+        wants = ctx.needs_input_grad
+        return (*scan_backward(*saved(), dy, _dense(dlast), ctx.la_step, wants[2], *wants[5:8]), None, None, None)
+
+
+def _scan_sizes(x, A, B):
+    if x.dim() < 2 or A.dim() != 2 or B.dim() not in (x.dim(), x.dim() + 1):
+        raise ValueError("x must be [..., N, C], A [C, states], B and C [..., N, states] or [..., N, groups, states]")
+    N, C = x.shape[-2:]
+    return x.numel() // (N * C) if x.numel() else 0, N, C, A.shape[1], B.shape[-2] if B.dim() > x.dim() else 1
+
+
+def scan_backward(x, dt, A, B, C, D, bias, lengths, saved, dy, dlast, step, wants_A, wants_D, wants_bias, wants_h0):
+    sizes = _scan_sizes(x, A, B)
+    dx, ddt = torch.empty_like(dy), torch.empty_like(dy)
+    dB, dC = (torch.empty(B.shape, dtype=B.dtype, device=x.device) for _ in range(2))
+    dA = torch.empty_like(A) if wants_A else None
+    dD = torch.empty_like(D) if wants_D else None
+    db = torch.empty_like(bias) if wants_bias else None
+    dh0 = torch.empty((*x.shape[:-2], *A.shape), dtype=torch.float32, device=x.device) if wants_h0 else None
+    ws = _bytes(_b.la_selective_workspace_bytes(*sizes, 1), x.device)
+    _b.la_selective_backward(x, dt, A, B, C, D, bias, saved, dy, dlast, dx, ddt, dA, dB, dC, dD, db, dh0, lengths, step, ws)
+    return dx, ddt, dA, dB, dC, dD, db, dh0
+
+
+def selective_scan(x, dt, A, B, C, D=None, bias=None, h0=None, lengths=None, step="softplus"):
+    """Differentiable selective state space scan along the second to last dimension of x, dt [..., N, C] (float32 or bfloat16
+    device tensors), with A [C, S] float32 and B, C [..., N, S], or [..., N, G, S] for G groups of channels, like x; all but A may be
+    parts of wider rows, which are read where they are:
+
+      h_t = exp(d_t A) h_{t-1} + d_t x_t B_t,  y_t = sum over the states C_t h_t + D x_t,  with
+      step "softplus":  d_t = log(1 + exp(dt_t + bias));   step "value":  d_t = dt_t + bias.
+
+    D, bias [C] float32 (None: zeros).  h0 [..., C, S] float32: the state before the first row (None: zeros).  lengths [...]
+    int32: rows from there on are padding, zero in every output.  Returns y like x and the state after the last row, [..., C, S]
+    float32, from which la_selective_step goes on.  For the backward pass it keeps its inputs and the states of every 16th row."""
+    if step not in _STEPS:
+        raise ValueError("steps are %s, got %r" % (" and ".join(map(repr, _STEPS)), step))
+    keeps = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, dt, A, B, C, D, bias, h0))
+    return SelectiveScanFunction.apply(x, dt, A, B, C, D, bias, h0, lengths, _STEPS[step], keeps)

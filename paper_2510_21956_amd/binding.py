@@ -26,6 +26,12 @@ LA_I8 = 3
 LA_GATE_VALUE = 0
 LA_GATE_SIGMOID = 1
 
+LA_ACT_NONE = 0
+LA_ACT_SILU = 1
+
+LA_STEP_VALUE = 0
+LA_STEP_SOFTPLUS = 1
+
 LA_MAX_TRACE = 8
 
 EXPORTS = ("la_version", "la_status_string", "la_workspace_bytes", "la_forward", "la_backward",
@@ -35,7 +41,9 @@ EXPORTS = ("la_version", "la_status_string", "la_workspace_bytes", "la_forward",
            "la_backward_qknorm", "la_forward_qknorm_save", "la_backward_qknorm_saved",
            "la_recurrence_workspace_bytes", "la_recurrence_forward", "la_recurrence_backward",
            "la_recurrence_step", "la_pack_rows", "la_pack_tensors", "la_unpack_rows", "la_rmsnorm_workspace_bytes",
-           "la_rmsnorm_forward", "la_rmsnorm_backward")
+           "la_rmsnorm_forward", "la_rmsnorm_backward", "la_conv_workspace_bytes", "la_conv_forward", "la_conv_backward",
+           "la_conv_step", "la_selective_workspace_bytes", "la_selective_saved_bytes", "la_selective_forward",
+           "la_selective_backward", "la_selective_step")
 
 
 class la_trace(ctypes.Structure):
@@ -127,6 +135,25 @@ def load_library():
     lib.la_rmsnorm_forward.argtypes = [vp] * 9 + [sz, i, f, i, i, i, i, vp]
     lib.la_rmsnorm_backward.restype = i
     lib.la_rmsnorm_backward.argtypes = [vp] * 8 + [sz, i, i, i, i, vp, sz, vp]
+    lib.la_conv_workspace_bytes.restype = sz
+    lib.la_conv_workspace_bytes.argtypes = [i] * 4
+    lib.la_conv_forward.restype = i
+    lib.la_conv_forward.argtypes = [vp, sz] + [vp] * 6 + [i] * 7 + [vp]
+    lib.la_conv_backward.restype = i
+    lib.la_conv_backward.argtypes = [vp, sz] + [vp] * 10 + [i] * 7 + [vp, sz, vp]
+    lib.la_conv_step.restype = i
+    lib.la_conv_step.argtypes = [vp, sz] + [vp] * 4 + [i] * 7 + [vp]
+    scan = [vp, sz, vp, sz, vp, vp, sz, vp, sz, vp, vp]  # x, dt, A, B, C and their strides, D, bias
+    lib.la_selective_workspace_bytes.restype = sz
+    lib.la_selective_workspace_bytes.argtypes = [i] * 6
+    lib.la_selective_saved_bytes.restype = sz
+    lib.la_selective_saved_bytes.argtypes = [i] * 4
+    lib.la_selective_forward.restype = i
+    lib.la_selective_forward.argtypes = scan + [vp] * 4 + [sz, vp] + [i] * 7 + [vp, sz, vp]
+    lib.la_selective_backward.restype = i
+    lib.la_selective_backward.argtypes = scan + [vp, sz] + [vp] * 11 + [i] * 7 + [vp, sz, vp]
+    lib.la_selective_step.restype = i
+    lib.la_selective_step.argtypes = scan + [vp] * 2 + [i] * 7 + [vp]
     lib.la_debug_override.restype = None
     lib.la_debug_override.argtypes = [i, i]
     _lib = lib
@@ -768,6 +795,185 @@ def la_rmsnorm_backward(total, scales, weight, rstd, dy, dtotal, dx, dweight, wo
     rows, C = _rows(dy)
     _call("la_rmsnorm_backward", dy, stream, (dx, dweight), _ptr(total), _ptr(scales), _ptr(weight), _ptr(rstd), _ptr(dy),
           _ptr(dtotal), _ptr(dx), _ptr(dweight), rows, C, dt, wt, dt if code is None else int(code), *_room(workspace))
+
+
+# ---- the selective state space layer ----------------------------------------------------------
+
+def row_stride(t, dims=1):
+    """Elements from one row of t to the next, a row being its last ``dims`` dimensions; None where rows are not dense, or do not
+    follow one another at one distance, at least their own length."""
+    row, step, sizes, strides = 1, None, t.shape, t.stride()
+    for d in reversed(range(len(sizes) - dims, len(sizes))):
+        if sizes[d] != 1 and strides[d] != row:
+            return None
+        row *= sizes[d]
+    behind = None
+    for d in reversed(range(len(sizes) - dims)):
+        if sizes[d] == 1:
+            continue
+        if step is None:
+            step = strides[d]
+        elif strides[d] != behind:
+            return None
+        behind = strides[d] * sizes[d]
+    step = row if step is None else step
+    return step if step >= row else None
+
+
+def _strided(ref, dims=1, **ts):
+    """The row strides of device tensors on ref's device."""
+    out = []
+    for name, t in ts.items():
+        if not t.is_cuda or t.get_device() != ref.get_device():
+            raise ValueError("tensors must be device tensors on one device")
+        step = row_stride(t, dims)
+        if step is None:
+            raise ValueError("the rows of %s must be dense and at one distance from one another" % name)
+        out.append(step)
+    return out
+
+
+def la_conv_workspace_bytes(B, N, C, W):
+    if max(B, N, C, W) >= _INTS:
+        return 0
+    return int(load_library().la_conv_workspace_bytes(B, N, C, W))
+
+
+def _conv(x, weight, bias, y, lengths, **states):
+    """Checks what the calls share; the row stride of x, its sizes, and the codes of the types."""
+    _check_tensors(weight, bias, y, lengths, *states.values())
+    stride, = _strided(weight, x=x)
+    B, N, C = _sequences(x)
+    if weight.dim() != 2 or weight.shape[0] != C:
+        raise ValueError("the weight must be [%d, taps], got %s" % (C, tuple(weight.shape)))
+    W = weight.shape[1]
+    _fit(W=W)
+    if weight.dtype not in (torch.float32, x.dtype):
+        raise TypeError("the weight must be float32 or %s, got %s" % (x.dtype, weight.dtype))
+    if bias is not None and (bias.shape != weight.shape[:1] or bias.dtype != weight.dtype):
+        raise ValueError("the bias must be [%d], of the weight's type" % C)
+    _like(x, y=y)
+    shape = (*x.shape[:-2], W - 1, C)
+    for name, t in states.items():
+        if t is not None and (t.shape != shape or t.dtype != x.dtype):
+            raise ValueError("%s must be %s %s" % (name, x.dtype, tuple(shape)))
+    return stride, (B, N, C, W), (_real_code(x), LA_F32 if weight.dtype == torch.float32 else LA_BF16)
+
+
+def la_conv_forward(x, weight, bias, state, y, last, lengths, act, stream=None):
+    """la_conv_forward of include/la.h: x, y [..., N, C] float32 or bfloat16, x a part of wider rows where wanted; weight [C, W],
+    bias [C] (or None) float32 or x's type; state, last [..., W - 1, C] like x, or None; lengths [...] int32 or None; act LA_ACT_NONE
+    or LA_ACT_SILU."""
+    _needed(x=x, weight=weight, y=y)
+    stride, sizes, codes = _conv(x, weight, bias, y, lengths, state=state, last=last)
+    _call("la_conv_forward", x, stream, (y, last), _ptr(x), stride, _ptr(weight), _ptr(bias), _ptr(state), _ptr(y), _ptr(last),
+          _lengths_ptr(lengths, x), *sizes, int(act), *codes)
+
+
+def la_conv_backward(x, weight, bias, state, dy, dlast, dx, dweight, dbias, dstate, lengths, act, workspace, stream=None):
+    """la_conv_backward of include/la.h (see la_conv_forward): dy, dx [..., N, C]; dlast, dstate [..., W - 1, C] like x, or None;
+    dweight [C, W], dbias [C] float32, or None; workspace: uint8 device tensor of la_conv_workspace_bytes(...) bytes where one of
+    these is given."""
+    _needed(x=x, weight=weight, dy=dy, dx=dx)
+    _check_tensors(weight, dx, dweight, dbias, workspace)
+    stride, sizes, codes = _conv(x, weight, bias, dy, lengths, state=state, dlast=dlast, dstate=dstate)
+    _like(x, dx=dx)
+    for name, t, shape in (("dweight", dweight, weight.shape), ("dbias", dbias, weight.shape[:1])):
+        if t is not None and (t.shape != shape or t.dtype != torch.float32):
+            raise ValueError("%s must be float32 %s" % (name, tuple(shape)))
+    _call("la_conv_backward", x, stream, (dx, dweight, dbias, dstate), _ptr(x), stride, _ptr(weight), _ptr(bias), _ptr(state),
+          _ptr(dy), _ptr(dlast), _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(dstate), _lengths_ptr(lengths, x), *sizes, int(act),
+          *codes, *_room(workspace))
+
+
+def la_conv_step(x, weight, bias, state, y, act, stream=None):
+    """la_conv_step of include/la.h: x, y [..., T, C]; state [..., W - 1, C] like x, updated in place (as a change that autograd
+    sees, and outside of any graph)."""
+    _needed(x=x, weight=weight, state=state, y=y)
+    stride, sizes, codes = _conv(x, weight, bias, y, None, state=state)
+    _call("la_conv_step", x, stream, (y, state), _ptr(x), stride, _ptr(weight), _ptr(bias), _ptr(state), _ptr(y), *sizes, int(act),
+          *codes)
+
+
+def la_selective_workspace_bytes(B, N, C, S, G, is_backward):
+    if max(B, N, C, S, G) >= _INTS:
+        return 0
+    return int(load_library().la_selective_workspace_bytes(B, N, C, S, G, int(bool(is_backward))))
+
+
+def la_selective_saved_bytes(B, N, C, S):
+    if max(B, N, C, S) >= _INTS:
+        return 0
+    return int(load_library().la_selective_saved_bytes(B, N, C, S))
+
+
+def _selective(x, dt, A, Bm, Cm, D, bias, lengths, states, like):
+    """Checks what the calls share; the arguments from x to bias, and the sizes."""
+    _needed(x=x, dt=dt, A=A, B=Bm, C=Cm)
+    _check_tensors(A, D, bias, lengths, *states.values(), *like.values())
+    xs, ts = _strided(A, x=x, dt=dt)
+    B, N, C = _sequences(x)
+    _like(x, dt=dt, **like)
+    if A.dim() != 2 or A.shape[0] != C or A.dtype != torch.float32:
+        raise ValueError("A must be float32 [%d, states]" % C)
+    S = A.shape[1]
+    if Bm.shape == (*x.shape[:-1], S):
+        G = 1
+    elif Bm.dim() == x.dim() + 1 and Bm.shape[:-2] == x.shape[:-1] and Bm.shape[-1] == S:
+        G = Bm.shape[-2]
+    else:
+        raise ValueError("B must be %s with the states, and groups before them where there are several" % (tuple(x.shape[:-1]),))
+    if Cm.shape != Bm.shape:
+        raise ValueError("C must be %s, got %s" % (tuple(Bm.shape), tuple(Cm.shape)))
+    if Bm.dtype != x.dtype or Cm.dtype != x.dtype:
+        raise TypeError("B and C must be %s" % x.dtype)
+    bs, cs = _strided(A, 1 if Bm.dim() == x.dim() else 2, B=Bm, C=Cm)
+    _fit(S=S, G=G)
+    for name, t in (("D", D), ("bias", bias)):
+        if t is not None and (t.shape != (C,) or t.dtype != torch.float32):
+            raise ValueError("%s must be float32 [%d]" % (name, C))
+    for name, t in states.items():
+        if t is not None and (t.shape != (*x.shape[:-2], C, S) or t.dtype != torch.float32):
+            raise ValueError("%s must be float32 %s" % (name, (*x.shape[:-2], C, S)))
+    return ((_ptr(x), xs, _ptr(dt), ts, _ptr(A), _ptr(Bm), bs, _ptr(Cm), cs, _ptr(D), _ptr(bias)), (B, N, C, S, G))
+
+
+def la_selective_forward(x, dt, A, Bm, Cm, D, bias, h0, y, last, saved, lengths, step, workspace, stream=None):
+    """la_selective_forward of include/la.h: x, dt, y [..., N, C], Bm, Cm [..., N, S] or [..., N, G, S] float32 or bfloat16, all but y
+    parts of wider rows where wanted; A [C, S], D, bias [C] (or None), h0, last [..., C, S] (or None) float32; saved: uint8 device
+    tensor of la_selective_saved_bytes(...) bytes where a backward call follows, or None; lengths [...] int32 or None; step
+    LA_STEP_VALUE or LA_STEP_SOFTPLUS; workspace: uint8 device tensor of la_selective_workspace_bytes(..., 0) bytes (None where that
+    is 0)."""
+    _needed(y=y)
+    head, sizes = _selective(x, dt, A, Bm, Cm, D, bias, lengths, {"h0": h0, "last": last}, {"y": y})
+    _check_tensors(A, saved, workspace)
+    _call("la_selective_forward", x, stream, (y, last, saved), *head, _ptr(h0), _ptr(y), _ptr(last), *_room(saved),
+          _lengths_ptr(lengths, x), *sizes, int(step), _real_code(x), *_room(workspace))
+
+
+def la_selective_backward(x, dt, A, Bm, Cm, D, bias, saved, dy, dlast, dx, ddt, dA, dB, dC, dD, dbias, dh0, lengths, step, workspace,
+                          stream=None):
+    """la_selective_backward of include/la.h (see la_selective_forward): saved as that call left it; dy, dx, ddt [..., N, C], dB, dC like
+    Bm, dense; dA, dD, dbias like A, D, bias, dlast, dh0 [..., C, S] float32, or None."""
+    _needed(saved=saved, dy=dy, dx=dx, ddt=ddt, dB=dB, dC=dC)
+    head, sizes = _selective(x, dt, A, Bm, Cm, D, bias, lengths, {"dlast": dlast, "dh0": dh0}, {"dy": dy, "dx": dx, "ddt": ddt})
+    _check_tensors(A, saved, dA, dB, dC, dD, dbias, workspace)
+    _like(Bm, dB=dB, dC=dC)
+    _like(A, dA=dA)
+    for name, t in (("dD", dD), ("dbias", dbias)):
+        if t is not None and (t.shape != A.shape[:1] or t.dtype != torch.float32):
+            raise ValueError("%s must be float32 [%d]" % (name, A.shape[0]))
+    _call("la_selective_backward", x, stream, (dx, ddt, dA, dB, dC, dD, dbias, dh0), *head, *_room(saved), _ptr(dy), _ptr(dlast),
+          _ptr(dx), _ptr(ddt), _ptr(dA), _ptr(dB), _ptr(dC), _ptr(dD), _ptr(dbias), _ptr(dh0), _lengths_ptr(lengths, x), *sizes,
+          int(step), _real_code(x), *_room(workspace))
+
+
+def la_selective_step(x, dt, A, Bm, Cm, D, bias, state, y, step, stream=None):
+    """la_selective_step of include/la.h: x, dt, y [..., T, C], Bm, Cm [..., T, S] or [..., T, G, S]; state [..., C, S] float32, updated
+    in place (as a change that autograd sees, and outside of any graph)."""
+    _needed(state=state, y=y)
+    head, sizes = _selective(x, dt, A, Bm, Cm, D, bias, None, {"state": state}, {"y": y})
+    _call("la_selective_step", x, stream, (y, state), *head, _ptr(state), _ptr(y), *sizes, int(step), _real_code(x))
 
 
 def in_native_code(name, where, *args):

@@ -22,6 +22,7 @@
 // row t-1.
 #include "la_checks.h"
 #include "la_common.h"
+#include "la_scalar.h"
 
 namespace la {
 namespace {
@@ -69,23 +70,12 @@ __device__ __forceinline__ void leave(void *row, unsigned channel, const float (
     } else __builtin_memcpy(p, &c, sizeof c);
 }
 
-// f and 1 - f of a stored gate, both from the smaller one's exponential: neither loses digits to a difference,
-// and infinite gates give 0 and 1.  The exponential's argument in base 2 is rounded, an error of up to |g| U
-// relative to it: float32 adds what the rounding lost, bfloat16 rounds to 2^-8 what that is far below.
+// f and 1 - f of a stored gate.
 template <int GATE, bool FINE>
 __device__ __forceinline__ void open_gate(float g, float &f, float &rest)
 {
     if (GATE == LA_GATE_SIGMOID) {
-        constexpr float L = 1.44269504f, Lrest = 1.92596299e-8f, ln2 = 0.693147181f;  // log2(e) in two parts
-        const float y = -fabsf(g), t = y * L;
-        float E = __builtin_amdgcn_exp2f(t);
-        if (FINE) {
-            const float lost = fmaf(y, Lrest, fmaf(y, L, -t));
-            E = fmaf(E, (y > -128.f ? lost : 0.f) * ln2, E);
-        }
-        const float large = __builtin_amdgcn_rcpf(1.f + E), small = E * large;
-        f = g >= 0.f ? large : small;
-        rest = g >= 0.f ? small : large;
+        sigmoid<FINE>(g, f, rest);
     } else {
         f = g;
         rest = 1.f;
