@@ -13,11 +13,11 @@ namespace la {
 namespace {
 
 constexpr int kMostStates = 128;
-constexpr int kRows = 16;  // of a tile
-// What the backward pass keeps of kCells / P rows, h and exp(d A) of every row and state, fills 128 registers, and its 64
-// sums over a wave's channels of either kind are one to a lane.  Where a tile has more rows they are taken in
-// parts, the states before a part formed once more from those before the tile.
-constexpr int kCells = 64;
+constexpr int kRows = 16, kPairs = kRows / 2;  // of a tile
+// What the backward pass keeps of kCells / P rows, h and exp(d A) of every row and state: 64 registers, and its 64
+// sums over a wave's channels, of either kind, are folded together.  Where a tile has more rows they are taken in parts,
+// the states before a part formed once more from those before the tile.
+constexpr int kCells = 32;
 
 struct Scan {
     const void *X, *Dt, *Bm, *Cm;
@@ -30,9 +30,9 @@ struct Scan {
     const int *lengths;
     const void *dY;
     void *dX, *dDt;
-    float *shares;       // [B, columns, tiles, W, parts, 2, 64] sums over a column's channels for dB, dC
+    float *shares;       // [B, columns, tiles, W, parts, 2, kCells] sums over a column's channels for dB, dC
     float *dA, *dd;      // [B * segs, S, C], [B * segs, 2, C] a segment's sums for dA; for dD and dbias
-    float *sums, *spans; // [B, segs, S, C] what a segment makes of zero states, [B, segs, C] the sum of its d
+    float *sums, *spans; // [B, segs, S, C] what a segment makes of zero states, then the states it starts from; [B, segs, C] the sum of its d
     int B, N, C, S, G, group, per, columns;  // channels of a group; columns of 64 channels to it, in all
     int tiles, seg, segs;                    // tiles of the sequence; rows of a segment, segments
     int step;
@@ -40,7 +40,8 @@ struct Scan {
 
 // Where a workgroup is: its sequence, channels and rows.
 struct Spot {
-    int b, column, g, c, seg, n, r0, r1;
+    int b, column, g, seg, n, r0, r1;
+    unsigned c;
     bool live;
     __device__ __forceinline__ Spot(const Scan &a, int lane)
     {
@@ -48,13 +49,43 @@ struct Spot {
         seg = (int)(blockIdx.x % a.segs);
         column = (int)(k % a.columns), b = (int)(k / a.columns);
         g = column / a.per;
-        c = g * a.group + column % a.per * 64 + lane;
-        const int behind = (g + 1) * a.group;
-        live = c < behind;
-        c = min(c, behind - 1);  // lanes behind the group's last channel read that one
-        n = a.lengths ? min(max(a.lengths[b], 0), a.N) : a.N;
+        const int mine = g * a.group + column % a.per * 64 + lane, behind = (g + 1) * a.group;
+        live = mine < behind;
+        c = (unsigned)min(mine, behind - 1);  // lanes behind the group's last channel read that one
+        n = a.lengths ? min(max(__builtin_amdgcn_readfirstlane(a.lengths[b]), 0), a.N) : a.N;
         r0 = min(seg * a.seg, a.N);
         r1 = min(n, r0 + a.seg);
+    }
+};
+
+// The rows of a tensor from the tile's first on, by a buffer's descriptor: a scalar address, a scalar offset of the row and a
+// lane's place in it in 32 bits, so that no lane adds up addresses.  (The descriptor is not asked to check: rows are
+// clamped to those that there are.)
+template <typename T>
+struct Rows {
+    char *tile;
+    unsigned stride, lane;  // bytes
+    __device__ __forceinline__ Rows(const void *p, size_t row, size_t stride, size_t column, unsigned lane)
+        : tile((char *)p + (row * stride + column) * sizeof(T)), stride((unsigned)(stride * sizeof(T))), lane(lane * (unsigned)sizeof(T))
+    {
+    }
+    __device__ __forceinline__ void move(int tiles) { tile += (ptrdiff_t)tiles * kRows * (ptrdiff_t)stride; }
+    __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer() const
+    {
+        return __builtin_amdgcn_make_buffer_rsrc(tile, 0, 0x7fffffff, 0x00020000);
+    }
+    __device__ __forceinline__ T operator[](int row) const
+    {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer(), lane, row * stride, 0));
+        else return __builtin_amdgcn_raw_buffer_load_b16(buffer(), lane, row * stride, 0);
+    }
+    __device__ __forceinline__ void put(int row, float x) const
+    {
+        if constexpr (sizeof(T) == 4) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(x), buffer(), lane, row * stride, 0);
+        else {
+            const __bf16 c = (__bf16)x;
+            __builtin_amdgcn_raw_buffer_store_b16(__builtin_bit_cast(short, c), buffer(), lane, row * stride, 0);
+        }
     }
 };
 
@@ -70,30 +101,91 @@ __device__ __forceinline__ float step_of(float dt, int step, float &slope)
     return softplus_of(dt, E);
 }
 
-// A tile's B and C on their way to LDS: R rows of [B | C], P W of each, zeros behind the last state and row.
-template <typename T, int P, int W, int R>
-struct Vectors {
-    static constexpr int COUNT = 2 * R * P / 64;
-    T v[COUNT];
-    __device__ __forceinline__ void load(const Scan &a, const Spot &p, int t)
+// What stands before it in the source comes before what stands behind it: the compiler would ask for all of a tile's rows first
+// and hold them in registers.
+__device__ __forceinline__ void keep_order()
+{
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+}
+
+// x is there here, and not where it is used: what it was made from is let go of.
+__device__ __forceinline__ void settle(float &x) { asm volatile("" : "+v"(x)); }
+
+// f(0), f(1), .. as constants.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        each<N, I + 1>(f);
+    }
+}
+
+// B or C of a tile for the P states of a wave: value P row + state stands in lane (P row + state) % 16 of every 16 lanes of a
+// register, from where the instruction that needs it reads it for all of them; zeros behind the last state and row.
+template <typename T, int P>
+struct Vector {
+    static constexpr int REGS = kRows * P / 16, STEP = 16 / P;  // rows of a register
+    Rows<T> from;
+    uint32_t mask;
+    int row;
+    uint32_t raw[REGS];
+    float v[REGS];
+    __device__ __forceinline__ Vector(const void *p, size_t row0, size_t stride, const Scan &a, const Spot &s, int wave, int lane)
+        : from(p, row0, stride, (size_t)s.g * a.S, 0)
     {
+        const int k = lane % 16, state = wave * P + k % P;
+        mask = state < a.S ? 0xffffffffu : 0;
+        row = k / P;
+        from.lane = (unsigned)row * from.stride + (unsigned)min(state, a.S - 1) * (unsigned)sizeof(T);
+    }
+    // rows: how many of the tile's there are
+    __device__ __forceinline__ void request(int rows)
+    {
+        if (rows >= kRows) {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) {
-            const int k = threadIdx.x + i * 64 * W, row = k / (2 * P * W), s = k % (P * W);
-            const bool c = k % (2 * P * W) >= P * W;
-            v[i] = (T)0;
-            if (s < a.S && t + row < p.n) {
-                const size_t r = (size_t)p.b * a.N + t + row;
-                v[i] = c ? ((const T *)a.Cm)[r * a.cs + p.g * a.S + s] : ((const T *)a.Bm)[r * a.bs + p.g * a.S + s];
+            for (int i = 0; i < REGS; ++i) raw[i] = widen(from[STEP * i]);
+        } else {
+#pragma unroll
+            for (int i = 0; i < REGS; ++i) {
+                raw[i] = 0;
+                if (STEP * i + row < rows) raw[i] = widen(from[STEP * i]);
             }
         }
     }
-    __device__ __forceinline__ void leave(float *to) const
+    static __device__ __forceinline__ uint32_t widen(float x) { return __float_as_uint(x); }
+    static __device__ __forceinline__ uint32_t widen(bf16_t x) { return x; }
+    __device__ __forceinline__ void arrive()
     {
 #pragma unroll
-        for (int i = 0; i < COUNT; ++i) to[threadIdx.x + i * 64 * W] = load_elem(v, i);
+        for (int i = 0; i < REGS; ++i) v[i] = __uint_as_float((sizeof(T) == 4 ? raw[i] : raw[i] << 16) & mask);
     }
 };
+// The value of lane K of 16.
+template <int K>
+__device__ __forceinline__ float of_lane(float v)
+{
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + K, 0xf, 0xf, true));
+}
+// acc_j += v_{K+j} x, and acc += sum_j v_{K+j} x_j, v_k being the value of lane k of 16.  (A register that another lane's value is
+// read from is ready two instructions after it was written.)
+#define LA_FMA_OF_LANE(acc, x, k) "v_fmac_f32_dpp " acc ", %[v], " x " row_newbcast:" k " row_mask:0xf bank_mask:0xf\n\t"
+template <int K, int P, int J = 0>
+__device__ __forceinline__ void fma_each(float (&acc)[P], float v, float x)
+{
+    asm("s_nop 1\n\t" LA_FMA_OF_LANE("%0", "%[x]", "%[k0]") LA_FMA_OF_LANE("%1", "%[x]", "%[k1]")
+        : "+v"(acc[J]), "+v"(acc[J + 1]) : [v] "v"(v), [x] "v"(x), [k0] "n"(K + J), [k1] "n"(K + J + 1));
+    if constexpr (J + 2 < P) fma_each<K, P, J + 2>(acc, v, x);
+}
+template <int K, int P, int J = 0>
+__device__ __forceinline__ void fma_all(float &acc, float v, const float (&x)[P])
+{
+    asm("s_nop 1\n\t" LA_FMA_OF_LANE("%0", "%[x0]", "%[k0]") LA_FMA_OF_LANE("%0", "%[x1]", "%[k1]")
+        : "+v"(acc) : [v] "v"(v), [x0] "v"(x[J]), [x1] "v"(x[J + 1]), [k0] "n"(K + J), [k1] "n"(K + J + 1));
+    if constexpr (J + 2 < P) fma_all<K, P, J + 2>(acc, v, x);
+}
+#undef LA_FMA_OF_LANE
 
 template <int P>
 __device__ __forceinline__ void decays(const Scan &a, const Spot &p, int wave, float (&A)[P])
@@ -104,13 +196,17 @@ __device__ __forceinline__ void decays(const Scan &a, const Spot &p, int wave, f
         A[j] = s < a.S ? a.A[(size_t)p.c * a.S + s] * kLog2e : 0.f;
     }
 }
+// The states that the walk starts from: the caller's, or those that k_selective_chain left for the segment.
 template <int P>
-__device__ __forceinline__ void states_from(const float *from, const Scan &a, const Spot &p, int wave, float (&h)[P])
+__device__ __forceinline__ void states_from(const Scan &a, const Spot &p, int wave, float (&h)[P])
 {
 #pragma unroll
     for (int j = 0; j < P; ++j) {
         const int s = wave * P + j;
-        h[j] = from && p.live && s < a.S ? from[((size_t)p.b * a.C + p.c) * a.S + s] : 0.f;
+        h[j] = 0.f;
+        if (!p.live || s >= a.S) continue;
+        if (a.segs > 1) h[j] = a.sums[(((size_t)p.b * a.segs + p.seg) * a.S + s) * a.C + p.c];
+        else if (a.first) h[j] = a.first[((size_t)p.b * a.C + p.c) * a.S + s];
     }
 }
 template <int P>
@@ -123,18 +219,41 @@ __device__ __forceinline__ void states_to(float *to, const Scan &a, const Spot &
         if (s < a.S) to[((size_t)p.b * a.C + p.c) * a.S + s] = h[j];
     }
 }
-// The states that the segments before (BWD: behind) this one leave.
-template <int P, bool BWD>
-__device__ __forceinline__ void walk_segments(const Scan &a, const Spot &p, int wave, const float (&A)[P], float (&h)[P])
+template <int P>
+__device__ __forceinline__ void leave_sums(const Scan &a, const Spot &p, int wave, const float (&h)[P], float span)
 {
-    const int end = BWD ? (p.n + a.seg - 1) / a.seg - 1 : 0;  // the last segment with rows
-    for (int k = end; BWD ? k > p.seg : k < p.seg; k += BWD ? -1 : 1) {
-        const size_t at = (size_t)p.b * a.segs + k;
-        const float span = a.spans[at * a.C + p.c];
+    if (!p.live) return;
+    const size_t at = (size_t)p.b * a.segs + p.seg;
 #pragma unroll
-        for (int j = 0; j < P; ++j) {
-            const int s = wave * P + j;
-            if (s < a.S) h[j] = fmaf(__builtin_amdgcn_exp2f(span * A[j]), h[j], a.sums[(at * a.S + s) * a.C + p.c]);
+    for (int j = 0; j < P; ++j)
+        if (wave * P + j < a.S) a.sums[(at * a.S + wave * P + j) * a.C + p.c] = h[j];
+    if (wave == 0) a.spans[at * a.C + p.c] = span;
+}
+
+// The states that every segment starts from, in place of what it makes of zero states: a lane to a state of a channel.
+template <bool BWD>
+__global__ void __launch_bounds__(256) k_selective_chain(Scan a)
+{
+    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    if (i >= (size_t)a.B * a.S * a.C) return;
+    const int c = (int)(i % a.C), s = (int)(i / a.C % a.S), b = (int)(i / a.C / a.S);
+    const float A = a.A[(size_t)c * a.S + s] * kLog2e;
+    float h = a.first ? a.first[((size_t)b * a.C + c) * a.S + s] : 0.f;
+    constexpr int AHEAD = 16;  // segments whose words are asked for together
+    for (int k0 = 0; k0 < a.segs; k0 += AHEAD) {
+        float own[AHEAD], span[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            const int k = min(k0 + i, a.segs - 1);
+            const size_t at = (size_t)b * a.segs + (BWD ? a.segs - 1 - k : k);
+            own[i] = a.sums[(at * a.S + s) * a.C + c], span[i] = a.spans[at * a.C + c];
+        }
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) {
+            if (k0 + i >= a.segs) break;
+            const size_t at = (size_t)b * a.segs + (BWD ? a.segs - 1 - k0 - i : k0 + i);
+            a.sums[(at * a.S + s) * a.C + c] = h;
+            h = fmaf(__builtin_amdgcn_exp2f(span[i] * A), h, own[i]);
         }
     }
 }
@@ -143,75 +262,113 @@ __device__ __forceinline__ void walk_segments(const Scan &a, const Spot &p, int 
 template <typename T, int P, int W, bool FULL>
 __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
 {
-    constexpr int R = kRows, OWN = (R + W - 1) / W;  // rows of a tile, of a wave
-    __shared__ float2 du[R][64];
-    __shared__ float ys[W][R][64];
-    __shared__ __align__(16) float bc[R][2][P * W];
+    constexpr int OWN = (kPairs + W - 1) / W;  // pairs of rows that a wave prepares
+    __shared__ float4 du[kPairs][64];
+    __shared__ float2 ys[FULL ? W : 1][kPairs][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Spot p(a, lane);
     float A[P], h[P], span = 0.f;
     decays<P>(a, p, wave, A);
-    states_from<P>(FULL ? a.first : nullptr, a, p, wave, h);
-    if (FULL) walk_segments<P, false>(a, p, wave, A, h);
+    if (FULL) states_from<P>(a, p, wave, h);
+    else
+#pragma unroll
+        for (int j = 0; j < P; ++j) h[j] = 0.f;
     const float bias = a.bias ? a.bias[p.c] : 0.f, D = a.D ? a.D[p.c] : 0.f;
-    T x[OWN], dt[OWN];
-    Vectors<T, P, W, R> vec;
-    auto request = [&](int t) {
+    const size_t row0 = (size_t)p.b * a.N + p.r0;
+    Rows<T> X(a.X, row0, a.xs, 0, p.c), Dt(a.Dt, row0, a.ts, 0, p.c), Y(a.Y, row0, a.C, 0, p.c);
+    Vector<T, P> B(a.Bm, row0, a.bs, a, p, wave, lane), C(a.Cm, row0, a.cs, a, p, wave, lane);
+    float *saved = a.saved ? a.saved + (((size_t)p.b * a.tiles + p.r0 / kRows) * a.S + wave * P) * a.C : nullptr;
+    T x[OWN][2], dt[OWN][2];
+    auto request = [&](int rows) {
 #pragma unroll
         for (int i = 0; i < OWN; ++i) {
-            const int r = wave + i * W;
-            if (R % W && r >= R) break;
-            const size_t row = (size_t)p.b * a.N + min(t + r, p.n - 1);
-            x[i] = ((const T *)a.X)[row * a.xs + p.c];
-            dt[i] = ((const T *)a.Dt)[row * a.ts + p.c];
-        }
-        vec.load(a, p, t);
-    };
-    if (p.r0 < p.r1) request(p.r0);
-    for (int t = p.r0; t < p.r1; t += R) {
-        float xw[OWN];
+            const int q = wave + i * W;
+            if (kPairs % W && q >= kPairs) break;
 #pragma unroll
-        for (int i = 0; i < OWN; ++i) {
-            const int r = wave + i * W;
-            if (R % W && r >= R) break;
-            float slope;
-            const float d = t + r < p.n ? step_of<sizeof(T) == 4>(load_elem(dt, i) + bias, a.step, slope) : 0.f;
-            xw[i] = t + r < p.n ? load_elem(x, i) : 0.f;
-            du[r][lane] = make_float2(d, d * xw[i]);
-        }
-        vec.leave(&bc[0][0][0]);
-        block_sync();
-        if (t + R < p.r1) request(t + R);
-        if (FULL && a.saved && p.live) {
-            float *to = a.saved + ((size_t)p.b * a.tiles + t / R) * a.S * a.C + p.c;
-#pragma unroll
-            for (int j = 0; j < P; ++j)
-                if (wave * P + j < a.S) to[(size_t)(wave * P + j) * a.C] = h[j];
-        }
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-            const float2 s = du[r][lane];
-            const float *Bt = &bc[r][0][wave * P], *Ct = &bc[r][1][wave * P];
-            float y = 0.f;
-#pragma unroll
-            for (int j = 0; j < P; ++j) {
-                h[j] = fmaf(__builtin_amdgcn_exp2f(s.x * A[j]), h[j], s.y * Bt[j]);
-                if (FULL) y = fmaf(Ct[j], h[j], y);
+            for (int r = 0; r < 2; ++r) {
+                const int row = min(2 * q + r, rows - 1);
+                x[i][r] = X[row], dt[i][r] = Dt[row];
             }
-            if (FULL) ys[wave][r][lane] = y;
-            else span += s.x;
         }
+        B.request(rows);
+        if (FULL) C.request(rows);
+    };
+    if (p.r0 < p.r1) request(p.r1 - p.r0);
+    for (int t = p.r0; t < p.r1; t += kRows) {
+        const int rows = p.r1 - t;
+        float xw[OWN][2];
+#pragma unroll
+        for (int i = 0; i < OWN; ++i) {
+            const int q = wave + i * W;
+            if (kPairs % W && q >= kPairs) break;
+            float d[2];
+#pragma unroll
+            for (int r = 0; r < 2; ++r) {
+                float slope;
+                d[r] = step_of<sizeof(T) == 4>(load_elem(dt[i], r) + bias, a.step, slope);
+                xw[i][r] = load_elem(x[i], r);
+                if (2 * q + r >= rows) d[r] = xw[i][r] = 0.f;
+            }
+            du[q][lane] = make_float4(d[0], d[0] * xw[i][0], d[1], d[1] * xw[i][1]);
+        }
+        B.arrive();
+        if (FULL) C.arrive();
+        block_sync();
+        if (rows > kRows) {
+            X.move(1), Dt.move(1), B.from.move(1), C.from.move(1);
+            request(rows - kRows);
+        }
+        if (FULL && a.saved) {
+            if (p.live)
+#pragma unroll
+                for (int j = 0; j < P; ++j)
+                    if (wave * P + j < a.S) saved[(size_t)j * a.C + p.c] = h[j];
+            saved += (size_t)a.S * a.C;
+        }
+        float4 s = du[0][lane], next = du[1][lane];
+        float f[2 * P], g[2 * P];  // exp(d A) of a pair of rows, and of the next
+        auto open = [&](float (&f)[2 * P], const float4 &s) {
+#pragma unroll
+            for (int j = 0; j < 2 * P; ++j) f[j] = __builtin_amdgcn_exp2f((j < P ? s.x : s.z) * A[j % P]);
+        };
+        open(f, s);
+        each<kPairs>([&](auto q_) {
+            constexpr int q = decltype(q_)::value;
+            const float4 after = du[q + 2 < kPairs ? q + 2 : kPairs - 1][lane];
+            float y[2] = {0.f, 0.f};
+            if constexpr (q + 1 < kPairs) open(g, next);
+            each<2>([&](auto r_) {
+                constexpr int r = decltype(r_)::value, k = (2 * q + r) * P;
+                each<P>([&](auto j) {
+                    h[j] = fmaf(f[r * P + j], h[j], (r ? s.w : s.y) * of_lane<k % 16 + decltype(j)::value>(B.v[k / 16]));
+                });
+                if (FULL) fma_all<k % 16>(y[r], C.v[k / 16], h);
+                else span += r ? s.z : s.x;
+            });
+            if (FULL) ys[wave][q][lane] = make_float2(y[0], y[1]);
+            s = next, next = after;
+#pragma unroll
+            for (int j = 0; j < 2 * P; ++j) f[j] = g[j];
+            keep_order();
+        });
         block_sync();
         if (FULL) {
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
-                const int r = wave + i * W;
-                if (R % W && r >= R) break;
-                float y = D * xw[i];
+                const int q = wave + i * W;
+                if (kPairs % W && q >= kPairs) break;
+                float y[2] = {D * xw[i][0], D * xw[i][1]};
 #pragma unroll
-                for (int w = 0; w < W; ++w) y += ys[w][r][lane];
-                if (p.live && t + r < p.n) store_elem((T *)a.Y, ((size_t)p.b * a.N + t + r) * a.C + p.c, y);
+                for (int w = 0; w < W; ++w) {
+                    const float2 v = ys[w][q][lane];
+                    y[0] += v.x, y[1] += v.y;
+                }
+                if (p.live) {
+                    if (2 * q < rows) Y.put(2 * q, y[0]);
+                    if (2 * q + 1 < rows) Y.put(2 * q + 1, y[1]);
+                }
             }
+            Y.move(1);
         }
     }
     if (FULL) {
@@ -219,166 +376,225 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
             for (int t = max(p.r0, p.n) + wave; t < min(a.N, p.r0 + a.seg); t += W)  // padding
                 store_elem((T *)a.Y, ((size_t)p.b * a.N + t) * a.C + p.c, 0.f);
         if (p.seg == max(p.n - 1, 0) / a.seg) states_to<P>(a.end, a, p, wave, h);
-    } else if (p.live) {
-        const size_t at = (size_t)p.b * a.segs + p.seg;
-#pragma unroll
-        for (int j = 0; j < P; ++j)
-            if (wave * P + j < a.S) a.sums[(at * a.S + wave * P + j) * a.C + p.c] = h[j];
-        if (wave == 0) a.spans[at * a.C + p.c] = span;
-    }
+    } else leave_sums<P>(a, p, wave, h, span);
 }
 
-// 64 values a lane, added up over the lanes: lane l gets the sum of value l.  Halves, then quarters of the values are
-// exchanged between the lanes' halves and quarters, so that every step halves what a lane has to add.
-__device__ __forceinline__ float over_lanes(float (&v)[64], int lane)
+// 64 values a lane, added up over the wave's lanes.  At every step a lane keeps half of its values, by a bit of its
+// number, and adds the partner's share of them, so that 64 sums take a lane 63 additions and not 6 each.  First the partners
+// within 16 lanes (rotated by 8, mirrored in 8), whose shares the additions read in place, the kept half chosen by
+// the instruction's mask of banks; then halves and quarters of the wave change places, one instruction for two values; the
+// last four values are added up over four neighbours.  Lane l ends with values 32 l3 + 16 l2 + 8 l5 + 4 l4 + (0 .. 3), l3 being bit 3
+// of l.  An instruction that reads another lane's register needs two others behind the one that wrote it.
+__device__ __forceinline__ float4 over_lanes(float (&v)[64])
 {
 #pragma unroll
-    for (int m = 32; m >= 1; m /= 2) {
-        const bool up = lane & m;
+    for (int i = 0; i < 32; ++i)
+        asm("s_nop 1\n\tv_add_f32_dpp %0, %1, %1 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %0, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xc"
+            : "=&v"(v[i]) : "v"(v[i]), "v"(v[i + 32]));
 #pragma unroll
-        for (int i = 0; i < m; ++i) {
-            const float keep = up ? v[i + m] : v[i], send = up ? v[i] : v[i + m];
-            v[i] = keep + __shfl_xor(send, m);
-        }
+    for (int i = 0; i < 16; ++i)
+        asm("s_nop 1\n\tv_add_f32_dpp %0, %1, %1 row_half_mirror row_mask:0xf bank_mask:0xf\n\t"
+            "v_add_f32_dpp %0, %2, %2 row_half_mirror row_mask:0xf bank_mask:0xa"
+            : "=&v"(v[i]) : "v"(v[i]), "v"(v[i + 16]));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 8]), false, false);
+        v[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
     }
-    return v[0];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const auto s = __builtin_amdgcn_permlane16_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 4]), false, false);
+        v[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);
+        v[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v[i]), 0xb1, 0xf, 0xf, true));
+        v[i] += __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v[i]), 0x4e, 0xf, 0xf, true));
+    }
+    return make_float4(v[0], v[1], v[2], v[3]);
 }
 
 // Backward.  FULL: outputs, walking the tiles from the far end: states from the saved ones before the tile on, then the rows in
 // reverse.  Else what the segment hands to the rows before it from nothing behind it.
 template <typename T, int P, int W, bool FULL>
-__global__ void __launch_bounds__(64 * W) k_selective_back(Scan a)
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(FULL ? (W == 12 || W == 6 ? 3 : W == 16 || W == 8 ? 4 : 3) : 4))) k_selective_back(Scan a)
 {
-    constexpr int R = kRows, OWN = (R + W - 1) / W, PART = kCells / P;
-    __shared__ float2 du[R][64];
-    __shared__ float dys[R][64];
-    __shared__ float2 gs[FULL ? W : 1][R][64];
-    __shared__ __align__(16) float bc[R][2][P * W];
+    constexpr int OWN = (kPairs + W - 1) / W, PART = kCells / P, PARTS = kRows / PART;
+    __shared__ float4 du[kPairs][64];
+    __shared__ float2 dys[kPairs][64];
+    __shared__ float4 gs[FULL ? W : 1][kPairs][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Spot p(a, lane);
     float A[P], carry[P], dA[P], before[P], dD = 0.f, db = 0.f, span = 0.f;
     decays<P>(a, p, wave, A);
+    if (FULL) states_from<P>(a, p, wave, carry);
 #pragma unroll
-    for (int j = 0; j < P; ++j) dA[j] = 0.f;
-    states_from<P>(FULL ? a.first : nullptr, a, p, wave, carry);
-    if (FULL) walk_segments<P, true>(a, p, wave, A, carry);
+    for (int j = 0; j < P; ++j) {
+        dA[j] = 0.f;
+        if (!FULL) carry[j] = 0.f;
+    }
     const float bias = a.bias ? a.bias[p.c] : 0.f, D = a.D ? a.D[p.c] : 0.f;
-    T x[OWN], dt[OWN], dy[OWN];
-    Vectors<T, P, W, R> vec;
-    auto request = [&](int t) {
+    const int tiles = p.r0 < p.r1 ? (p.r1 - p.r0 + kRows - 1) / kRows : 0, last = p.r0 + max(tiles - 1, 0) * kRows;
+    const size_t row0 = (size_t)p.b * a.N + last;
+    Rows<T> X(a.X, row0, a.xs, 0, p.c), Dt(a.Dt, row0, a.ts, 0, p.c), dY(a.dY, row0, a.C, 0, p.c), dX(a.dX, row0, a.C, 0, p.c), dDt(a.dDt, row0, a.C, 0, p.c);
+    Vector<T, P> B(a.Bm, row0, a.bs, a, p, wave, lane), C(a.Cm, row0, a.cs, a, p, wave, lane);
+    const float *saved = a.saved + (((size_t)p.b * a.tiles + last / kRows) * a.S + wave * P) * a.C;
+    float *shares = a.shares + ((((size_t)p.b * a.columns + p.column) * a.tiles + last / kRows) * W + wave) * PARTS * 64;
+    T x[OWN][2], dt[OWN][2], dy[OWN][2];
+    auto request = [&](int rows) {
 #pragma unroll
         for (int i = 0; i < OWN; ++i) {
-            const int r = wave + i * W;
-            if (R % W && r >= R) break;
-            const size_t row = (size_t)p.b * a.N + min(t + r, p.n - 1);
-            if (FULL) x[i] = ((const T *)a.X)[row * a.xs + p.c];
-            dt[i] = ((const T *)a.Dt)[row * a.ts + p.c];
-            dy[i] = ((const T *)a.dY)[row * a.C + p.c];
-        }
-        vec.load(a, p, t);
-        if (FULL) {
-            const float *from = a.saved + ((size_t)p.b * a.tiles + t / R) * a.S * a.C + p.c;
+            const int q = wave + i * W;
+            if (kPairs % W && q >= kPairs) break;
 #pragma unroll
-            for (int j = 0; j < P; ++j) before[j] = p.live && wave * P + j < a.S ? from[(size_t)(wave * P + j) * a.C] : 0.f;
+            for (int r = 0; r < 2; ++r) {
+                const int row = min(2 * q + r, rows - 1);
+                if (FULL) x[i][r] = X[row];
+                dt[i][r] = Dt[row], dy[i][r] = dY[row];
+            }
         }
+        if (FULL) B.request(rows);
+        C.request(rows);
+        if (FULL)
+#pragma unroll
+            for (int j = 0; j < P; ++j) before[j] = p.live && wave * P + j < a.S ? saved[(size_t)j * a.C + p.c] : 0.f;
     };
-    const int last = p.r0 + (p.r1 - p.r0 - 1) / R * R;
-    if (p.r0 < p.r1) request(last);
-    for (int t = last; p.r0 < p.r1 && t >= p.r0; t -= R) {
-        float xw[OWN], slope[OWN];
+    // lanes without a channel of their own have no share in the sums over channels
+    const uint32_t mask = p.live ? 0xffffffffu : 0;
+    auto of_live = [&](float v) { return __uint_as_float(__float_as_uint(v) & mask); };
+    if (tiles) request(p.r1 - last);
+    for (int k = 0, rows = p.r1 - last; k < tiles; ++k, rows = kRows) {
+        float xw[OWN][2], slope[OWN][2];
 #pragma unroll
         for (int i = 0; i < OWN; ++i) {
-            const int r = wave + i * W;
-            if (R % W && r >= R) break;
-            const bool here = p.live && t + r < p.n;
-            const float d = step_of<sizeof(T) == 4>(load_elem(dt, i) + bias, a.step, slope[i]);
-            xw[i] = FULL && here ? load_elem(x, i) : 0.f;
-            du[r][lane] = make_float2(here ? d : 0.f, here ? d * xw[i] : 0.f);
-            dys[r][lane] = here ? load_elem(dy, i) : 0.f;
-        }
-        vec.leave(&bc[0][0][0]);
-        block_sync();
-        if constexpr (FULL) {
-            float begin[P];
+            const int q = wave + i * W;
+            if (kPairs % W && q >= kPairs) break;
+            float d[2], y[2];
 #pragma unroll
-            for (int j = 0; j < P; ++j) begin[j] = before[j];
-            if (t > p.r0) request(t - R);
-            float *to = a.shares + ((((size_t)p.b * a.columns + p.column) * a.tiles + t / R) * W + wave) * (R / PART) * 128;
-#pragma unroll 1
-            for (int r0 = R - PART; r0 >= 0; r0 -= PART) {
-                float h[kCells], f[kCells], h0[P];
-#pragma unroll
-                for (int j = 0; j < P; ++j) h0[j] = begin[j];
-                for (int r = 0; r < r0; ++r) {
-                    const float2 s = du[r][lane];
-#pragma unroll
-                    for (int j = 0; j < P; ++j) h0[j] = fmaf(__builtin_amdgcn_exp2f(s.x * A[j]), h0[j], s.y * bc[r][0][wave * P + j]);
-                }
-#pragma unroll
-                for (int r = 0; r < PART; ++r) {
-                    const float2 s = du[r0 + r][lane];
-                    const float *Bt = &bc[r0 + r][0][wave * P];
-#pragma unroll
-                    for (int j = 0; j < P; ++j) {
-                        f[r * P + j] = __builtin_amdgcn_exp2f(s.x * A[j]);
-                        h[r * P + j] = fmaf(f[r * P + j], r ? h[(r - 1) * P + j] : h0[j], s.y * Bt[j]);
-                    }
-                }
-#pragma unroll
-                for (int r = PART - 1; r >= 0; --r) {
-                    const float2 s = du[r0 + r][lane];
-                    const float y = dys[r0 + r][lane];
-                    const float *Bt = &bc[r0 + r][0][wave * P], *Ct = &bc[r0 + r][1][wave * P];
-                    float gu = 0.f, gd = 0.f;
-#pragma unroll
-                    for (int j = 0; j < P; ++j) {
-                        const float g = fmaf(Ct[j], y, carry[j]);
-                        gu = fmaf(g, Bt[j], gu);
-                        carry[j] = g * f[r * P + j];
-                        const float e = carry[j] * (r ? h[(r - 1) * P + j] : h0[j]);
-                        gd = fmaf(e, A[j], gd);
-                        dA[j] = fmaf(e, s.x, dA[j]);
-                        f[r * P + j] = g * s.y;
-                        h[r * P + j] *= y;
-                    }
-                    gs[wave][r0 + r][lane] = make_float2(gu, gd * kLn2);
-                }
-                to[r0 / PART * 128 + lane] = over_lanes(f, lane);
-                to[r0 / PART * 128 + 64 + lane] = over_lanes(h, lane);
+            for (int r = 0; r < 2; ++r) {
+                d[r] = step_of<sizeof(T) == 4>(load_elem(dt[i], r) + bias, a.step, slope[i][r]);
+                xw[i][r] = FULL ? of_live(load_elem(x[i], r)) : 0.f;
+                y[r] = of_live(load_elem(dy[i], r));
+                if (2 * q + r >= rows) d[r] = xw[i][r] = y[r] = 0.f;
             }
+            du[q][lane] = make_float4(d[0], d[0] * xw[i][0], d[1], d[1] * xw[i][1]);
+            dys[q][lane] = make_float2(y[0], y[1]);
+        }
+        if (FULL) B.arrive();
+        C.arrive();
+        float begin[P];
+#pragma unroll
+        for (int j = 0; j < P; ++j) begin[j] = FULL ? before[j] : 0.f;
+        block_sync();
+        if (k + 1 < tiles) {
+            X.move(-1), Dt.move(-1), dY.move(-1), B.from.move(-1), C.from.move(-1);
+            saved -= (size_t)a.S * a.C;
+            request(kRows);
+        }
+        if constexpr (FULL) {
+            each<PARTS>([&](auto part_) {
+                constexpr int part = PARTS - 1 - decltype(part_)::value, first = part * PART / 2;  // pair
+                float v[64], h0[P], own[P];  // f: exp(d A), then shares of dB; h, then shares of dC
+                float *const f = v, *const h = v + kCells;
+#pragma unroll
+                for (int j = 0; j < P; ++j) h0[j] = begin[j], own[j] = 0.f;
+                each<first>([&](auto q_) {
+                    constexpr int q = decltype(q_)::value;
+                    const float4 s = du[q][lane];
+                    each<2 * P>([&](auto i) {
+                        constexpr int r = decltype(i)::value / P, j = decltype(i)::value % P, k = (2 * q + r) * P + j;
+                        h0[j] = fmaf(__builtin_amdgcn_exp2f((r ? s.z : s.x) * A[j]), h0[j], (r ? s.w : s.y) * of_lane<k % 16>(B.v[k / 16]));
+                    });
+                    if (q % 2) keep_order();
+                });
+                float4 s = du[first][lane];
+                each<PART / 2>([&](auto q_) {
+                    constexpr int q = decltype(q_)::value;
+                    const float4 next = du[first + (q + 1 < PART / 2 ? q + 1 : q)][lane];
+                    each<2 * P>([&](auto i) {
+                        constexpr int r = decltype(i)::value / P, j = decltype(i)::value % P, k = (2 * q + r) * P + j, at = k + 2 * first * P;
+                        f[k] = __builtin_amdgcn_exp2f((r ? s.z : s.x) * A[j]);
+                        h[k] = fmaf(f[k], k >= P ? h[k - P] : h0[j], (r ? s.w : s.y) * of_lane<at % 16>(B.v[at / 16]));
+                        settle(f[k]), settle(h[k]);
+                    });
+                    s = next;
+                    keep_order();
+                });
+                float2 y2 = dys[first + PART / 2 - 1][lane];
+                each<PART / 2>([&](auto q_) {
+                    constexpr int q = PART / 2 - 1 - decltype(q_)::value;
+                    const float4 next = du[first + (q ? q - 1 : q)][lane];
+                    const float2 nexty = dys[first + (q ? q - 1 : q)][lane];
+                    float gu[2] = {0.f, 0.f}, gd[2] = {0.f, 0.f};
+                    each<2>([&](auto r_) {
+                        constexpr int r = 1 - decltype(r_)::value, k = (2 * q + r) * P, at = k + 2 * first * P;
+                        const float d = r ? s.z : s.x, u = r ? s.w : s.y, y = r ? y2.y : y2.x;
+                        fma_each<at % 16>(carry, C.v[at / 16], y);
+                        fma_all<at % 16>(gu[r], B.v[at / 16], carry);
+#pragma unroll
+                        for (int j = 0; j < P; ++j) {
+                            const float g = carry[j];
+                            carry[j] = g * f[k + j];
+                            const float e = carry[j] * (k ? h[k - P + j] : h0[j]);
+                            gd[r] = fmaf(e, A[j], gd[r]);
+                            own[j] = fmaf(e, d, own[j]);
+                            f[k + j] = g * u;
+                            h[k + j] *= y;
+                            settle(f[k + j]), settle(h[k + j]), settle(own[j]), settle(carry[j]);
+                        }
+                    });
+                    gs[wave][first + q][lane] = make_float4(gu[0], gd[0] * kLn2, gu[1], gd[1] * kLn2);
+                    s = next, y2 = nexty;
+                    keep_order();
+                });
+#pragma unroll
+                for (int j = 0; j < P; ++j) dA[j] += own[j];
+                const float4 sum = over_lanes(v);
+                if (lane % 4 == 0)
+                    *(float4 *)(shares + part * 64 + (lane & 8) * 4 + (lane & 4) * 4 + (lane & 32) / 4 + (lane & 16) / 4) = sum;
+            });
+            shares -= W * PARTS * 64;
         } else {
-            if (t > p.r0) request(t - R);
+            each<kPairs>([&](auto q_) {
+                constexpr int q = kPairs - 1 - decltype(q_)::value;
+                const float4 s = du[q][lane];
+                const float2 y = dys[q][lane];
+                each<2>([&](auto r_) {
+                    constexpr int r = 1 - decltype(r_)::value, k = (2 * q + r) * P;
+                    fma_each<k % 16>(carry, C.v[k / 16], r ? y.y : y.x);
 #pragma unroll
-            for (int r = R - 1; r >= 0; --r) {
-                const float2 s = du[r][lane];
-                const float y = dys[r][lane];
-                const float *Ct = &bc[r][1][wave * P];
-#pragma unroll
-                for (int j = 0; j < P; ++j) carry[j] = fmaf(Ct[j], y, carry[j]) * __builtin_amdgcn_exp2f(s.x * A[j]);
-                span += s.x;
-            }
+                    for (int j = 0; j < P; ++j) carry[j] *= __builtin_amdgcn_exp2f((r ? s.z : s.x) * A[j]);
+                    span += r ? s.z : s.x;
+                });
+            });
         }
         block_sync();
         if constexpr (FULL) {
+            float dDt_ = 0.f, db_ = 0.f;
 #pragma unroll
             for (int i = 0; i < OWN; ++i) {
-                const int r = wave + i * W;
-                if (R % W && r >= R) break;
-                float gu = 0.f, gd = 0.f;
+                const int q = wave + i * W;
+                if (kPairs % W && q >= kPairs) break;
+                float4 g = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
                 for (int w = 0; w < W; ++w) {
-                    const float2 g = gs[w][r][lane];
-                    gu += g.x, gd += g.y;
+                    const float4 o = gs[w][q][lane];
+                    g.x += o.x, g.y += o.y, g.z += o.z, g.w += o.w;
                 }
-                const float y = dys[r][lane], dd = fmaf(xw[i], gu, gd) * slope[i];
-                if (p.live && t + r < p.n) {
-                    const size_t at = ((size_t)p.b * a.N + t + r) * a.C + p.c;
-                    store_elem((T *)a.dX, at, fmaf(du[r][lane].x, gu, D * y));
-                    store_elem((T *)a.dDt, at, dd);
-                    dD = fmaf(y, xw[i], dD);
-                    db += dd;
+                const float4 s = du[q][lane];
+                const float2 y2 = dys[q][lane];
+#pragma unroll
+                for (int r = 0; r < 2; ++r) {
+                    const float gu = r ? g.z : g.x, gd = r ? g.w : g.y, y = r ? y2.y : y2.x;
+                    const float dd = fmaf(xw[i][r], gu, gd) * slope[i][r];
+                    if (p.live && 2 * q + r < rows) {
+                        dX.put(2 * q + r, fmaf(r ? s.z : s.x, gu, D * y));
+                        dDt.put(2 * q + r, dd);
+                        dDt_ = fmaf(y, xw[i][r], dDt_);
+                        db_ += dd;
+                    }
                 }
             }
+            dD += dDt_, db += db_;
+            dX.move(-1), dDt.move(-1);
         }
     }
     const size_t at = (size_t)p.b * a.segs + p.seg;
@@ -391,7 +607,7 @@ __global__ void __launch_bounds__(64 * W) k_selective_back(Scan a)
             }
         if (p.seg == 0) states_to<P>(a.end, a, p, wave, carry);
         block_sync();
-        gs[wave][0][lane] = make_float2(dD, db);
+        gs[wave][0][lane] = make_float4(dD, db, 0.f, 0.f);
         block_sync();
         if (!p.live) return;
         if (a.dA)
@@ -405,30 +621,25 @@ __global__ void __launch_bounds__(64 * W) k_selective_back(Scan a)
             a.dd[at * 2 * a.C + p.c] = s.x;
             a.dd[(at * 2 + 1) * a.C + p.c] = s.y;
         }
-    } else if (p.live) {
-#pragma unroll
-        for (int j = 0; j < P; ++j)
-            if (wave * P + j < a.S) a.sums[(at * a.S + wave * P + j) * a.C + p.c] = carry[j];
-        if (wave == 0) a.spans[at * a.C + p.c] = span;
-    }
+    } else leave_sums<P>(a, p, wave, carry, span);
 }
 
 // dB and dC from the columns' shares: a lane to a value, the columns of a group in order.
-template <typename T, int P, int W>
-__global__ void __launch_bounds__(256) k_selective_vectors(Scan a, T *dB, T *dC)
+template <typename T>
+__global__ void __launch_bounds__(256) k_selective_shares(Scan a, T *dB, T *dC, int P, int W)
 {
-    constexpr int PART = kCells / P, EACH = W * (kRows / PART) * 128;  // values of a tile
-    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)a.B * a.G * a.tiles * EACH; i += (size_t)gridDim.x * 256) {
-        const size_t k = i / EACH;
-        const int v = (int)(i % EACH), m = v % 64, part = v / 128 % (kRows / PART), w = v / 128 / (kRows / PART);
+    const int part = kCells / P, parts = kRows / part, each = W * parts * 64;  // values of a tile
+    for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < (size_t)a.B * a.G * a.tiles * each; i += (size_t)gridDim.x * 256) {
+        const size_t k = i / each;
+        const int v = (int)(i - k * each), m = v % kCells, w = v / 64 / parts;
         const int tile = (int)(k % a.tiles), g = (int)(k / a.tiles % a.G), b = (int)(k / a.tiles / a.G);
-        const int t = tile * kRows + part * PART + m / P, s = w * P + m % P;
+        const int t = tile * kRows + v / 64 % parts * part + m / P, s = w * P + m % P;
         if (t >= a.N || s >= a.S) continue;
         const int n = a.lengths ? min(max(a.lengths[b], 0), a.N) : a.N;
         float sum = 0.f;
         if (t < n)
-            for (int c = 0; c < a.per; ++c) sum += a.shares[(((size_t)b * a.columns + g * a.per + c) * a.tiles + tile) * EACH + v];
-        store_elem(v % 128 < 64 ? dB : dC, (((size_t)b * a.N + t) * a.G + g) * a.S + s, sum);
+            for (int c = 0; c < a.per; ++c) sum += a.shares[(((size_t)b * a.columns + g * a.per + c) * a.tiles + tile) * each + v];
+        store_elem(v % 64 < kCells ? dB : dC, (((size_t)b * a.N + t) * a.G + g) * a.S + s, sum);
     }
 }
 
@@ -497,33 +708,34 @@ __global__ void __launch_bounds__(256) k_selective_step(Scan a, float *state, in
 struct Shape {
     int P, W;
 };
-Shape shape_of(int S)
+Shape shape_of(int S, bool two)
 {
-    if (S <= 32) return {4, S <= 4 ? 1 : S <= 8 ? 2 : S <= 12 ? 3 : S <= 16 ? 4 : S <= 24 ? 6 : 8};
-    if (S <= 64) return {8, S <= 48 ? 6 : 8};
-    return {16, S <= 96 ? 6 : 8};
+    if (S <= 8 || (S <= 16 && two)) return {2, S <= 2 ? 1 : S <= 4 ? 2 : S <= 8 ? 4 : S <= 12 ? 6 : 8};
+    if (S <= 64) return {4, S <= 16 ? 4 : S <= 24 ? 6 : S <= 32 ? 8 : S <= 48 ? 12 : 16};
+    return {8, S <= 96 ? 12 : 16};
 }
 // f(states as a constant, waves as a constant)
 template <typename F>
-void by_shape(int S, F f)
+void by_shape(const Shape &s, F f)
 {
-    const Shape s = shape_of(S);
     auto with = [&](auto P, auto W) {
         if (s.P == decltype(P)::value && s.W == decltype(W)::value) f(P, W);
     };
+    auto two = std::integral_constant<int, 2>();
     auto four = std::integral_constant<int, 4>();
     auto eight = std::integral_constant<int, 8>();
-    auto more = std::integral_constant<int, 16>();
-    with(four, std::integral_constant<int, 1>());
-    with(four, std::integral_constant<int, 2>());
-    with(four, std::integral_constant<int, 3>());
-    with(four, std::integral_constant<int, 4>());
+    with(two, std::integral_constant<int, 1>());
+    with(two, two);
+    with(two, four);
+    with(two, std::integral_constant<int, 6>());
+    with(two, eight);
+    with(four, four);
     with(four, std::integral_constant<int, 6>());
-    with(four, std::integral_constant<int, 8>());
-    with(eight, std::integral_constant<int, 6>());
-    with(eight, std::integral_constant<int, 8>());
-    with(more, std::integral_constant<int, 6>());
-    with(more, std::integral_constant<int, 8>());
+    with(four, eight);
+    with(four, std::integral_constant<int, 12>());
+    with(four, std::integral_constant<int, 16>());
+    with(eight, std::integral_constant<int, 12>());
+    with(eight, std::integral_constant<int, 16>());
 }
 
 la_status check_shape(int B, int N, int C, int S, int G)
@@ -539,6 +751,8 @@ la_status check(const Scan &a, la_step step, la_dtype dt)
     if (s != LA_OK) return s;
     const size_t vec = (size_t)a.G * a.S;
     if (a.xs < (size_t)a.C || a.ts < (size_t)a.C || a.bs < vec || a.cs < vec) return LA_ERR_SHAPE;
+    for (size_t n : {a.xs, a.ts, a.bs, a.cs, vec, (size_t)a.C})
+        if (n >= 1 << 24) return LA_ERR_SHAPE;  // rows of a tile in 32 bits
     for (size_t n : {a.xs, a.ts, a.bs, a.cs, vec})
         if ((double)a.B * a.N * (double)n >= 1099511627776.0) return LA_ERR_SHAPE;  // 2^40
     if (!real_type(dt) || (step != LA_STEP_VALUE && step != LA_STEP_SOFTPLUS)) return LA_ERR_UNSUPPORTED;
@@ -562,14 +776,35 @@ struct Inputs {
         r[7] = {a.first, (size_t)a.B * a.C * a.S * 4}, r[8] = {a.lengths, (size_t)a.B * 4};
     }
 };
-void lay_out(Scan &a)
+// How a call is laid out: the states of a wave, and the segments that sequences are cut into, whose start states two more launches
+// find (what every segment makes of zero states, an exponential and three operations for every row and state once more, and
+// the walk along the segments).  512 rows take, in us, with w waves on every SIMD of the busiest compute units (S = 16, bf16):
+// 39 + 29 w forward, 100 + 80 w backward, what the segments make of zero states 28 + 23 w and 31 + 21 w.  Segments fill the
+// compute units once forward, about twice backward (5 and 3 or 4 waves to a SIMD at once), and have 32 rows at least; one
+// piece where that takes less.  Of 1 to 96 segments, on 10 shapes of 1 to 256 chains, this takes 1.04 times the best on the average.
+// Forward, one piece and few waves: two states a wave instead of four, whose twice as many waves hide each other's
+// waits (8 x 2048 rows of 2048 channels 228 us, with four 260, in 8 segments 240).
+Shape lay_out(Scan &a, bool backward)
 {
     a.group = a.C / a.G;
     a.per = (a.group + 63) / 64;
     a.columns = a.G * a.per;
     a.tiles = (a.N + kRows - 1) / kRows;
-    a.seg = a.tiles * kRows;
-    a.segs = 1;
+    const Shape s = shape_of(a.S, false);
+    const double chains = (double)a.B * a.columns, waves = chains * s.W / 1024.0, rows = a.N / 512.0;
+    const int slots = 256 * ((backward ? s.W % 8 ? 12 : 16 : 20) / s.W);  // workgroups at once
+    const int rounds = (int)((backward ? 1792.0 : 1536.0) * 4 / s.W / slots + 0.4);
+    const double most = (rounds ? rounds : 1) * (double)slots / chains;
+    int segs = (int)(most < 256.0 ? most : 256.0);
+    if (segs > a.N / 32) segs = a.N / 32;
+    const double busiest = (double)(int)((chains + 255) / 256) * s.W / 4.0;
+    const double whole = rows * (backward ? 100 + 80 * busiest : 39 + 29 * busiest);
+    const double cut = 8.0 + rows * (backward ? 101 * waves + 131.0 / segs : 52 * waves + 67.0 / segs);
+    if (segs < 2 || whole <= cut) segs = 1;
+    const int of = (a.tiles + segs - 1) / segs;
+    a.seg = of * kRows;
+    a.segs = (a.tiles + of - 1) / of;
+    return shape_of(a.S, !backward && a.segs == 1 && waves < 2.0);
 }
 Scan scan_of(const void *X, size_t xs, const void *Dt, size_t ts, const float *A, const void *Bm, size_t bs, const void *Cm, size_t cs,
              const float *D, const float *bias, int B, int N, int C, int S, int G, la_step step)
@@ -580,13 +815,13 @@ Scan scan_of(const void *X, size_t xs, const void *Dt, size_t ts, const float *A
     return a;
 }
 
-// Floats of a tile's shares: kRows rows of the P W states of a workgroup, for dB and for dC.
-size_t shares_of(int S) { return (size_t)shape_of(S).P * shape_of(S).W * kRows * 2; }
+// Floats of a tile's shares of dB and dC.
+size_t shares_of(const Shape &s) { return (size_t)s.W * (kRows * s.P / kCells) * 64; }
 
 // What a call keeps in its workspace, in floats.
 struct Room {
     size_t shares, dA, dd, sums, spans, bytes;
-    Room(const Scan &a, bool back)
+    Room(const Scan &a, const Shape &shape, bool back)
     {
         size_t at = 0;
         auto take = [&](size_t n) {
@@ -598,13 +833,19 @@ struct Room {
         const bool cut = a.segs > 1;
         sums = take(cut ? segs * a.S * a.C : 0);
         spans = take(cut ? segs * a.C : 0);
-        shares = take(back ? (size_t)a.B * a.columns * a.tiles * shares_of(a.S) : 0);
+        shares = take(back ? (size_t)a.B * a.columns * a.tiles * shares_of(shape) : 0);
         dA = take(back ? segs * a.S * a.C : 0);
         dd = take(back ? segs * 2 * a.C : 0);
         bytes = at * 4;
     }
 };
 
+// Workgroups of 256 for n values, which walk the values where a grid would be too large.
+dim3 blocks_of(size_t n)
+{
+    const size_t k = (n + 255) / 256;
+    return dim3((unsigned)(k < 1 << 20 ? k : 1 << 20));
+}
 la_status done() { return hipGetLastError() == hipSuccess ? LA_OK : LA_ERR_LAUNCH; }
 
 }  // namespace
@@ -617,8 +858,8 @@ size_t la_selective_workspace_bytes(int B, int N, int C, int S, int G, int is_ba
     if (la::check_shape(B, N, C, S, G) != LA_OK) return 0;
     la::Scan a{};
     a.B = B, a.N = N, a.C = C, a.S = S, a.G = G;
-    la::lay_out(a);
-    return la::Room(a, is_backward != 0).bytes;
+    const la::Shape shape = la::lay_out(a, is_backward != 0);
+    return la::Room(a, shape, is_backward != 0).bytes;
 }
 
 size_t la_selective_saved_bytes(int B, int N, int C, int S)
@@ -638,8 +879,8 @@ la_status la_selective_forward(const void *X, size_t x_stride, const void *Dt, s
     const la_status s = la::check(a, step, dt);
     if (s != LA_OK) return s;
     if (!Y) return LA_ERR_NULL;
-    la::lay_out(a);
-    const la::Room room(a, false);
+    const la::Shape shape = la::lay_out(a, false);
+    const la::Room room(a, shape, false);
     const size_t kept = la_selective_saved_bytes(B, N, C, S);
     if (room.bytes && (!workspace || workspace_bytes < room.bytes || !la::aligned_to(workspace, 256))) return LA_ERR_WORKSPACE;
     if (saved && (saved_bytes < kept || !la::aligned_to(saved, 256))) return LA_ERR_WORKSPACE;
@@ -648,15 +889,21 @@ la_status la_selective_forward(const void *X, size_t x_stride, const void *Dt, s
     if (la::any_alias(in.r, 9, outs, 4)) return LA_ERR_ALIAS;
     if (hipPeekAtLastError() != hipSuccess) return LA_ERR_LAUNCH;
     a.sums = (float *)workspace + room.sums, a.spans = (float *)workspace + room.spans;
-    const dim3 grid((unsigned)((size_t)B * a.columns * a.segs));
+    const dim3 grid((unsigned)((size_t)B * a.columns * a.segs)), chain((unsigned)(((size_t)B * C * S + 255) / 256));
     const hipStream_t st = (hipStream_t)hip_stream;
-    la::by_shape(S, [&](auto P, auto W) {
+    la::by_shape(shape, [&](auto P, auto W) {
         constexpr int p = decltype(P)::value, w = decltype(W)::value;
         if (dt == LA_F32) {
-            if (a.segs > 1) la::k_selective<float, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+            if (a.segs > 1) {
+                la::k_selective<float, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective_chain<false><<<chain, dim3(256), 0, st>>>(a);
+            }
             la::k_selective<float, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
         } else {
-            if (a.segs > 1) la::k_selective<la::bf16_t, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+            if (a.segs > 1) {
+                la::k_selective<la::bf16_t, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective_chain<false><<<chain, dim3(256), 0, st>>>(a);
+            }
             la::k_selective<la::bf16_t, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
         }
     });
@@ -678,8 +925,8 @@ la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, 
     const size_t e = la::size_of(dt), tb = (size_t)B * N * C * e, vb = (size_t)B * N * G * S * e;
     if (!la::aligned_to(dBm, e) || !la::aligned_to(dCm, e) || !la::aligned_to(dA, 4) || !la::aligned_to(dD, 4) || !la::aligned_to(dbias, 4))
         return LA_ERR_ALIGN;
-    la::lay_out(a);
-    const la::Room room(a, true);
+    const la::Shape shape = la::lay_out(a, true);
+    const la::Room room(a, shape, true);
     const size_t kept = la_selective_saved_bytes(B, N, C, S);
     if (!workspace || workspace_bytes < room.bytes || !la::aligned_to(workspace, 256)) return LA_ERR_WORKSPACE;
     if (!saved || saved_bytes < kept || !la::aligned_to(saved, 256)) return LA_ERR_WORKSPACE;
@@ -694,22 +941,27 @@ la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, 
     float *const ws = (float *)workspace;
     a.sums = ws + room.sums, a.spans = ws + room.spans, a.shares = ws + room.shares;
     a.dA = dA ? ws + room.dA : nullptr, a.dd = ws + room.dd;
-    const dim3 grid((unsigned)((size_t)B * a.columns * a.segs));
+    const dim3 grid((unsigned)((size_t)B * a.columns * a.segs)), chain((unsigned)(((size_t)B * C * S + 255) / 256));
     const hipStream_t st = (hipStream_t)hip_stream;
-    la::by_shape(S, [&](auto P, auto W) {
+    la::by_shape(shape, [&](auto P, auto W) {
         constexpr int p = decltype(P)::value, w = decltype(W)::value;
-        const size_t values = ((size_t)B * G * a.tiles * la::shares_of(S) + 255) / 256;
-        const dim3 all((unsigned)(values < 1 << 20 ? values : 1 << 20));
         if (dt == LA_F32) {
-            if (a.segs > 1) la::k_selective_back<float, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+            if (a.segs > 1) {
+                la::k_selective_back<float, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective_chain<true><<<chain, dim3(256), 0, st>>>(a);
+            }
             la::k_selective_back<float, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
-            la::k_selective_vectors<float, p, w><<<all, dim3(256), 0, st>>>(a, (float *)dBm, (float *)dCm);
         } else {
-            if (a.segs > 1) la::k_selective_back<la::bf16_t, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+            if (a.segs > 1) {
+                la::k_selective_back<la::bf16_t, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective_chain<true><<<chain, dim3(256), 0, st>>>(a);
+            }
             la::k_selective_back<la::bf16_t, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
-            la::k_selective_vectors<la::bf16_t, p, w><<<all, dim3(256), 0, st>>>(a, (la::bf16_t *)dBm, (la::bf16_t *)dCm);
         }
     });
+    const dim3 all = la::blocks_of((size_t)B * G * a.tiles * la::shares_of(shape));
+    if (dt == LA_F32) la::k_selective_shares<float><<<all, dim3(256), 0, st>>>(a, (float *)dBm, (float *)dCm, shape.P, shape.W);
+    else la::k_selective_shares<la::bf16_t><<<all, dim3(256), 0, st>>>(a, (la::bf16_t *)dBm, (la::bf16_t *)dCm, shape.P, shape.W);
     if (dA || dD || dbias) la::k_selective_join<<<dim3((C + 63) / 64, S + 2), dim3(256), 0, st>>>(a, dA, dD, dbias);
     return la::done();
 }
