@@ -366,6 +366,9 @@ def causal_conv(x, weight, bias=None, state=None, lengths=None, activation="silu
     call's state go on."""
     if activation not in _ACTS:
         raise ValueError("activations are %s, got %r" % (" and ".join(map(repr, _ACTS)), activation))
+    out = _b.in_native_code("conv", "la_conv_forward", x, weight, bias, state, lengths, _ACTS[activation])
+    if out is not None:
+        return out
     return CausalConvFunction.apply(x, weight, bias, state, lengths, _ACTS[activation])
 
 
@@ -430,5 +433,8 @@ def selective_scan(x, dt, A, B, C, D=None, bias=None, h0=None, lengths=None, ste
     float32, from which la_selective_step goes on.  For the backward pass it keeps its inputs and the states of every 16th row."""
     if step not in _STEPS:
         raise ValueError("steps are %s, got %r" % (" and ".join(map(repr, _STEPS)), step))
+    out = _b.in_native_code("scan", "la_selective_forward", x, dt, A, B, C, D, bias, h0, lengths, _STEPS[step])
+    if out is not None:
+        return out
     keeps = torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (x, dt, A, B, C, D, bias, h0))
     return SelectiveScanFunction.apply(x, dt, A, B, C, D, bias, h0, lengths, _STEPS[step], keeps)

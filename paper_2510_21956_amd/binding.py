@@ -195,6 +195,9 @@ def _open_native(lib):
             lib.la_rmsnorm_backward, lib.la_forward_traced, lib.la_forward_qknorm, lib.la_forward_save,
             lib.la_forward_qknorm_save, lib.la_backward_saved, lib.la_backward_qknorm_saved, lib.la_workspace_bytes,
             lib.la_saved_state_bytes)))
+    module.init_scan(autograd.conv_backward, autograd.scan_backward, *(ctypes.cast(f, ctypes.c_void_p).value for f in (
+        lib.la_conv_workspace_bytes, lib.la_conv_forward, lib.la_conv_backward, lib.la_conv_step, lib.la_selective_workspace_bytes,
+        lib.la_selective_saved_bytes, lib.la_selective_forward, lib.la_selective_backward, lib.la_selective_step)))
     return module
 
 
@@ -809,14 +812,14 @@ def row_stride(t, dims=1):
         row *= sizes[d]
     behind = None
     for d in reversed(range(len(sizes) - dims)):
-        if sizes[d] == 1:
+        if sizes[d] == 1 or not t.numel():
             continue
         if step is None:
             step = strides[d]
         elif strides[d] != behind:
             return None
         behind = strides[d] * sizes[d]
-    step = row if step is None else step
+    step = row if step is None or not t.numel() else step
     return step if step >= row else None
 
 
@@ -831,6 +834,16 @@ def _strided(ref, dims=1, **ts):
             raise ValueError("the rows of %s must be dense and at one distance from one another" % name)
         out.append(step)
     return out
+
+
+def _natively(name, where, *args):
+    """Whether the call was made in native code (csrc/la_bind_scan.cpp)."""
+    if _native is None:
+        return False
+    rc = getattr(_native, name)(*args)
+    if rc:
+        raise LaError(rc, where)
+    return rc == 0
 
 
 def la_conv_workspace_bytes(B, N, C, W):
@@ -864,6 +877,8 @@ def la_conv_forward(x, weight, bias, state, y, last, lengths, act, stream=None):
     """la_conv_forward of include/la.h: x, y [..., N, C] float32 or bfloat16, x a part of wider rows where wanted; weight [C, W],
     bias [C] (or None) float32 or x's type; state, last [..., W - 1, C] like x, or None; lengths [...] int32 or None; act LA_ACT_NONE
     or LA_ACT_SILU."""
+    if _natively("conv_forward", "la_conv_forward", x, weight, bias, state, y, last, lengths, act, stream):
+        return
     _needed(x=x, weight=weight, y=y)
     stride, sizes, codes = _conv(x, weight, bias, y, lengths, state=state, last=last)
     _call("la_conv_forward", x, stream, (y, last), _ptr(x), stride, _ptr(weight), _ptr(bias), _ptr(state), _ptr(y), _ptr(last),
@@ -889,6 +904,8 @@ def la_conv_backward(x, weight, bias, state, dy, dlast, dx, dweight, dbias, dsta
 def la_conv_step(x, weight, bias, state, y, act, stream=None):
     """la_conv_step of include/la.h: x, y [..., T, C]; state [..., W - 1, C] like x, updated in place (as a change that autograd
     sees, and outside of any graph)."""
+    if _natively("conv_step", "la_conv_step", x, weight, bias, state, y, act, stream):
+        return
     _needed(x=x, weight=weight, state=state, y=y)
     stride, sizes, codes = _conv(x, weight, bias, y, None, state=state)
     _call("la_conv_step", x, stream, (y, state), _ptr(x), stride, _ptr(weight), _ptr(bias), _ptr(state), _ptr(y), *sizes, int(act),
@@ -944,6 +961,8 @@ def la_selective_forward(x, dt, A, Bm, Cm, D, bias, h0, y, last, saved, lengths,
     tensor of la_selective_saved_bytes(...) bytes where a backward call follows, or None; lengths [...] int32 or None; step
     LA_STEP_VALUE or LA_STEP_SOFTPLUS; workspace: uint8 device tensor of la_selective_workspace_bytes(..., 0) bytes (None where that
     is 0)."""
+    if _natively("scan_forward", "la_selective_forward", x, dt, A, Bm, Cm, D, bias, h0, y, last, saved, lengths, step, workspace, stream):
+        return
     _needed(y=y)
     head, sizes = _selective(x, dt, A, Bm, Cm, D, bias, lengths, {"h0": h0, "last": last}, {"y": y})
     _check_tensors(A, saved, workspace)
@@ -971,6 +990,8 @@ def la_selective_backward(x, dt, A, Bm, Cm, D, bias, saved, dy, dlast, dx, ddt, 
 def la_selective_step(x, dt, A, Bm, Cm, D, bias, state, y, step, stream=None):
     """la_selective_step of include/la.h: x, dt, y [..., T, C], Bm, Cm [..., T, S] or [..., T, G, S]; state [..., C, S] float32, updated
     in place (as a change that autograd sees, and outside of any graph)."""
+    if _natively("scan_step", "la_selective_step", x, dt, A, Bm, Cm, D, bias, state, y, step, stream):
+        return
     _needed(state=state, y=y)
     head, sizes = _selective(x, dt, A, Bm, Cm, D, bias, None, {"state": state}, {"y": y})
     _call("la_selective_step", x, stream, (y, state), *head, _ptr(state), _ptr(y), *sizes, int(step), _real_code(x))

@@ -352,6 +352,7 @@ PyMethodDef methods[] = {{"init", (PyCFunction)(void (*)())init, METH_FASTCALL, 
                          {"decode_step", (PyCFunction)(void (*)())decode_step, METH_FASTCALL, nullptr},
                          {"decode_prefill", (PyCFunction)(void (*)())decode_prefill, METH_FASTCALL, nullptr},
                          {"init_layer", (PyCFunction)(void (*)())init_layer, METH_FASTCALL, nullptr},
+                         {"init_scan", (PyCFunction)(void (*)())init_scan, METH_FASTCALL, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -361,6 +362,7 @@ PyMODINIT_FUNC PyInit__marshal()
 {
     PyObject *m = PyModule_Create(&module);
     if (m && PyModule_AddFunctions(m, layer_methods) < 0) Py_CLEAR(m);
+    if (m && PyModule_AddFunctions(m, scan_methods) < 0) Py_CLEAR(m);
     if (m && PyModule_AddStringConstant(m, "built_for", LA_BUILT_FOR) < 0) Py_CLEAR(m);
     return m;
 }

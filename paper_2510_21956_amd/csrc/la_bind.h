@@ -5,10 +5,13 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/ops/empty.h>
 #include <ATen/ops/empty_like.h>
+#include <c10/core/DeviceGuard.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_cpp_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/jit/frontend/tracer.h>
@@ -18,6 +21,8 @@
 extern PyObject *raw_stream;  // device index -> stream handle of its current stream (la_bind.cpp)
 PyObject *init_layer(PyObject *, PyObject *const *x, Py_ssize_t n);  // la_bind_layer.cpp
 extern PyMethodDef layer_methods[];
+PyObject *init_scan(PyObject *, PyObject *const *x, Py_ssize_t n);  // la_bind_scan.cpp
+extern PyMethodDef scan_methods[];
 
 namespace {
 
@@ -143,5 +148,96 @@ inline void *current_stream(const at::Tensor &ref) { return c10::hip::getCurrent
 struct Status {  // what the library answered
     int rc;
 };
+
+// ---- what the autograd nodes of the operators around the attention share ----------------------------------------
+
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
+typedef std::optional<at::Tensor> Maybe;
+
+inline void *data(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
+inline void *data(const Maybe &t) { return t ? t->data_ptr() : nullptr; }
+inline Maybe maybe(PyObject *o) { return is_none(o) ? Maybe() : Maybe(tensor(o)); }
+inline Maybe packed(const Maybe &t) { return t ? Maybe(t->contiguous()) : t; }
+inline at::Tensor kept(const Maybe &t) { return t ? *t : at::Tensor(); }
+
+// A tensor as the kernels take it, like ref (device, type and, where given, sizes).
+inline bool fits(const at::Tensor &t, const at::Tensor &ref, at::ScalarType type, at::IntArrayRef sizes)
+{
+    return !t.defined() || (t.is_cuda() && t.is_contiguous() && !t.unsafeGetTensorImpl()->is_python_dispatch() &&
+                            t.get_device() == ref.get_device() && t.scalar_type() == type && t.sizes() == sizes);
+}
+
+// Gradients of gradients are not defined: where a graph of the backward pass is asked for, its results come out of a node
+// that refuses, tied to all that they depend on (the operator's inputs and the incoming gradients), so that no
+// derivative goes past it.
+inline variable_list once(variable_list out, const variable_list &grads)
+{
+    using namespace torch::autograd;
+    if (!at::GradMode::is_enabled()) return out;
+    edge_list edges = collect_next_edges(grads);
+    if (const auto node = get_current_node()) edges.insert(edges.end(), node->next_edges().begin(), node->next_edges().end());
+    const auto refuse =
+        std::make_shared<Error>("gradients of gradients are not defined for this operator", std::move(edges));
+    for (at::Tensor &t : out)
+        if (t.defined()) set_history(t = t.detach(), refuse);
+    return out;
+}
+
+// Calls a backward pass in Python with `args` (a tuple, taken); its results, None where there is none.
+inline variable_list from_python(PyObject *f, PyObject *args)
+{
+    PyObject *got = args ? PyObject_CallObject(f, args) : nullptr;
+    Py_XDECREF(args);
+    if (!got) {
+        python_error e;
+        e.persist();
+        throw e;
+    }
+    variable_list out;
+    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(got); ++i) {
+        PyObject *o = PyTuple_GET_ITEM(got, i);
+        out.push_back(is_none(o) ? at::Tensor() : tensor(o));
+    }
+    Py_DECREF(got);
+    return out;
+}
+inline PyObject *wrapped(const at::Tensor &t)
+{
+    if (t.defined()) return THPVariable_Wrap(t);
+    Py_RETURN_NONE;
+}
+inline PyObject *tuple(const variable_list &ts)
+{
+    PyObject *out = PyTuple_New((Py_ssize_t)ts.size());
+    for (size_t i = 0; out && i < ts.size(); ++i) PyTuple_SET_ITEM(out, (Py_ssize_t)i, wrapped(ts[i]));
+    return out;
+}
+
+// Sizes that are the library's ints.
+inline bool ints(std::initializer_list<int64_t> sizes)
+{
+    return std::max(sizes) < (int64_t)1 << 31;
+}
+
+
+// What a call has written: a node that saved it must not go on with the new values.
+inline void written(std::initializer_list<PyObject *> ts)
+{
+    for (PyObject *o : ts)
+        if (!is_none(o) && !tensor(o).is_inference()) tensor(o).unsafeGetTensorImpl()->bump_version();
+}
+// Takes the entry points' addresses x[0 .. n - 1].
+inline bool addresses(PyObject *const *x, void **const *to, Py_ssize_t n)
+{
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        *to[i] = PyLong_AsVoidPtr(x[i]);
+        if (!*to[i]) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "null address");
+            return false;
+        }
+    }
+    return true;
+}
 
 }  // namespace

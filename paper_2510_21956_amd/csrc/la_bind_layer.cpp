@@ -3,17 +3,9 @@
 // stays with the Python functions of the same steps.  Through Python and here, us, nearly all of it host: rms_norm
 // on 5003 rows of 771, fp32, forward and backward 121 and 62; attention with checkpoints on 1 slice of 256 rows,
 // D = 16, 235 and 91; rms_norm_quantised on 8 rows 17 and 7.0; a step of a recurrence 8.3 and 4.0.
-#include <c10/core/DeviceGuard.h>
-#include <torch/csrc/autograd/functions/basic_ops.h>
-#include <torch/csrc/autograd/functions/utils.h>
-
 #include "la_bind.h"
 
 namespace {
-
-using torch::autograd::AutogradContext;
-using torch::autograd::variable_list;
-typedef std::optional<at::Tensor> Maybe;
 
 PyObject *python_recurrence, *python_norm, *python_checkpointed;  // the backward passes in Python
 
@@ -32,72 +24,7 @@ decltype(&la_backward_saved) att_backward, att_backward_qknorm;
 decltype(&la_workspace_bytes) att_bytes;
 decltype(&la_saved_state_bytes) att_saved_bytes;
 
-void *data(const at::Tensor &t) { return t.defined() ? t.data_ptr() : nullptr; }
-void *data(const Maybe &t) { return t ? t->data_ptr() : nullptr; }
-Maybe maybe(PyObject *o) { return is_none(o) ? Maybe() : Maybe(tensor(o)); }
-Maybe packed(const Maybe &t) { return t ? Maybe(t->contiguous()) : t; }
-at::Tensor kept(const Maybe &t) { return t ? *t : at::Tensor(); }
-
-// A tensor as the kernels take it, like ref (device, type and, where given, sizes).
-bool fits(const at::Tensor &t, const at::Tensor &ref, at::ScalarType type, at::IntArrayRef sizes)
-{
-    return !t.defined() || (t.is_cuda() && t.is_contiguous() && !t.unsafeGetTensorImpl()->is_python_dispatch() &&
-                            t.get_device() == ref.get_device() && t.scalar_type() == type && t.sizes() == sizes);
-}
-
-// Gradients of gradients are not defined: where a graph of the backward pass is asked for, its results come out of a node
-// that refuses, tied to all that they depend on (the operator's inputs and the incoming gradients), so that no
-// derivative goes past it.
-variable_list once(variable_list out, const variable_list &grads)
-{
-    using namespace torch::autograd;
-    if (!at::GradMode::is_enabled()) return out;
-    edge_list edges = collect_next_edges(grads);
-    if (const auto node = get_current_node()) edges.insert(edges.end(), node->next_edges().begin(), node->next_edges().end());
-    const auto refuse =
-        std::make_shared<Error>("gradients of gradients are not defined for this operator", std::move(edges));
-    for (at::Tensor &t : out)
-        if (t.defined()) set_history(t = t.detach(), refuse);
-    return out;
-}
-
-// Calls a backward pass in Python with `args` (a tuple, taken); its results, None where there is none.
-variable_list from_python(PyObject *f, PyObject *args)
-{
-    PyObject *got = args ? PyObject_CallObject(f, args) : nullptr;
-    Py_XDECREF(args);
-    if (!got) {
-        python_error e;
-        e.persist();
-        throw e;
-    }
-    variable_list out;
-    for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(got); ++i) {
-        PyObject *o = PyTuple_GET_ITEM(got, i);
-        out.push_back(is_none(o) ? at::Tensor() : tensor(o));
-    }
-    Py_DECREF(got);
-    return out;
-}
-PyObject *wrapped(const at::Tensor &t)
-{
-    if (t.defined()) return THPVariable_Wrap(t);
-    Py_RETURN_NONE;
-}
-PyObject *tuple(const variable_list &ts)
-{
-    PyObject *out = PyTuple_New((Py_ssize_t)ts.size());
-    for (size_t i = 0; out && i < ts.size(); ++i) PyTuple_SET_ITEM(out, (Py_ssize_t)i, wrapped(ts[i]));
-    return out;
-}
-
 // ---- gated recurrence -----------------------------------------------------------------------------------------
-
-// Sizes that are the library's ints.
-bool ints(std::initializer_list<int64_t> sizes)
-{
-    return std::max(sizes) < (int64_t)1 << 31;
-}
 
 struct Sequences {
     int B, N, C;

@@ -1,0 +1,329 @@
+"""The autograd nodes of the short convolution and the selective scan, in native code and in Python; calls on streams, in
+graphs, on tensors that are written in between; the two operators as a layer runs them."""
+import threading
+
+import pytest
+import torch
+
+import paper_2510_21956_amd as la
+from layer_reference import within
+from paper_2510_21956_amd import binding
+from selective_reference import Scan64, conv64
+
+pytestmark = pytest.mark.gpu
+
+
+def rand(*shape, seed=0, dtype=torch.float32):
+    return torch.randn(shape, device="cuda", generator=torch.Generator(device="cuda").manual_seed(seed)).to(dtype)
+
+
+NAMES = ["convolution", "convolution with a state", "weights in x's type", "bias without a gradient", "part of wider rows", "rows far apart",
+         "scan", "scan with a state", "groups", "scan of parts of wider rows", "state without a gradient", "decays without a gradient"]
+
+
+def calls(dtype):
+    x, dt, wide = rand(3, 70, 48, dtype=dtype), rand(3, 70, 48, seed=1, dtype=dtype), rand(3, 70, 100, seed=2, dtype=dtype)
+    w, b, st = rand(48, 4, seed=3), rand(48, seed=4), rand(3, 3, 48, seed=5, dtype=dtype)
+    A, Bm, Cm = -torch.exp(rand(48, 10, seed=6)), rand(3, 70, 10, seed=7, dtype=dtype), rand(3, 70, 10, seed=8, dtype=dtype)
+    B2, D, bias, h0 = rand(3, 70, 2, 10, seed=9, dtype=dtype), rand(48, seed=10), rand(48, seed=11), rand(3, 48, 10, seed=12)
+    n = torch.tensor([70, 0, 33], dtype=torch.int32, device="cuda")
+    return {
+        "convolution": (lambda x, w: la.causal_conv(x, w), [x, w]),
+        "convolution with a state": (lambda x, w, b, s: la.causal_conv(x, w, b, s, n, activation="none"), [x, w, b, st]),
+        "weights in x's type": (lambda x, w, b: la.causal_conv(x, w.to(x.dtype), b.to(x.dtype)), [x, w, b]),
+        "bias without a gradient": (lambda x, w, s: la.causal_conv(x, w, b, s), [x, w, st]),
+        "part of wider rows": (lambda v, w: la.causal_conv(v[..., 9:57], w), [wide, w]),
+        "rows far apart": (lambda v, w: la.causal_conv(v[:, ::2, :48], w), [wide, w]),
+        "scan": (lambda x, d, A, B, C: la.selective_scan(x, d, A, B, C), [x, dt, A, Bm, Cm]),
+        "scan with a state": (lambda x, d, A, B, C, D, b, h: la.selective_scan(x, d, A, B, C, D, b, h, n), [x, dt, A, Bm, Cm, D, bias, h0]),
+        "groups": (lambda x, d, A, B, D: la.selective_scan(x, d.abs(), A, B, B.flip(2), D, step="value"), [x, dt, A, B2, D]),
+        "scan of parts of wider rows": (lambda v, d, A, b: la.selective_scan(v[..., 1:49], d, A, v[..., 60:70], v[..., 90:], None, b), [wide, dt, A, bias]),
+        "state without a gradient": (lambda x, d, A, B, C: la.selective_scan(x, d, A, B, C, D, None, h0), [x, dt, A, Bm, Cm]),
+        "decays without a gradient": (lambda x, D, b: la.selective_scan(x, dt, A, Bm, Cm, D, b), [x, D, bias]),
+    }
+
+
+def run(f, inputs, alone=False):
+    ts = [t.clone().requires_grad_(True) for t in inputs]
+    shapes = []
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: shapes.append((tuple(t.shape), t.dtype)) or t.clone(), lambda t: t):
+        out = f(*ts)
+    used = out[-1:] if alone else out
+    grads = torch.autograd.grad(used, ts, [rand(*o.shape, seed=90 + k, dtype=o.dtype) for k, o in enumerate(used)], allow_unused=True)
+    return out, grads, sorted(map(str, shapes))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("name", NAMES)
+def test_native_and_python(monkeypatch, name, dtype):
+    every = calls(dtype)
+    assert list(every) == NAMES
+    f, inputs = every[name]
+    assert la.load_library() and binding._native is not None
+    native = [run(f, inputs, alone) for alone in (False, True)]
+    monkeypatch.setattr(binding, "_native", None)
+    for (o1, g1, s1), alone in zip(native, (False, True)):
+        o2, g2, s2 = run(f, inputs, alone)
+        assert len(o1) == len(o2) and all(torch.equal(a, b) for a, b in zip(o1, o2))
+        assert all((a is None) == (b is None) and (a is None or torch.equal(a, b)) for a, b in zip(g1, g2)), (name, alone)
+        assert s1 == s2, (name, s1, s2)
+
+
+def test_nothing_is_kept_without_gradients():
+    x, dt, A, B = rand(2, 300, 64), rand(2, 300, 64, seed=1), -torch.exp(rand(64, 16, seed=2)), rand(2, 300, 16, seed=3)
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: pytest.fail("kept") if t.requires_grad else t, lambda t: t):
+        y, last = la.selective_scan(x, dt, A, B, B)
+    assert not y.requires_grad
+    with torch.no_grad():
+        z, _ = la.selective_scan(x.requires_grad_(True), dt, A, B, B)
+    assert not z.requires_grad and torch.equal(y, z)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_calls_in_native_code_and_in_python(monkeypatch, native):
+    """The calls of a serving program, every optional argument there and missing."""
+    la.load_library()
+    if not native:
+        monkeypatch.setattr(binding, "_native", None)
+    x, w, b = rand(2, 20, 40, dtype=torch.bfloat16), rand(40, 4, seed=1), rand(40, seed=2)
+    n = torch.tensor([20, 7], dtype=torch.int32, device="cuda")
+    out = []
+    for bias, state, last, lengths in ((None, None, None, None), (b, rand(2, 3, 40, seed=3, dtype=torch.bfloat16), torch.empty(2, 3, 40, device="cuda", dtype=torch.bfloat16), n)):
+        y = torch.empty_like(x)
+        la.la_conv_forward(x, w, bias, state, y, last, lengths, la.LA_ACT_SILU)
+        out += [y, last]
+        if state is not None:
+            la.la_conv_step(x[:, :2].contiguous(), w, bias, state, y[:, :2].contiguous(), la.LA_ACT_NONE)
+            out.append(state)
+    A, B, D = -torch.exp(rand(40, 6, seed=4)), rand(2, 20, 2, 6, seed=5, dtype=torch.bfloat16), rand(40, seed=6)
+    ws = torch.empty(max(256, la.la_selective_workspace_bytes(2, 20, 40, 6, 2, 0)), dtype=torch.uint8, device="cuda")
+    for D_, bias, h0, last, lengths in ((None, None, None, None, None), (D, b, rand(2, 40, 6, seed=7), torch.empty(2, 40, 6, device="cuda"), n)):
+        y = torch.empty_like(x)
+        la.la_selective_forward(x, x, A, B, B, D_, bias, h0, y, last, None, lengths, la.LA_STEP_SOFTPLUS, ws)
+        out += [y, last]
+        if h0 is not None:
+            la.la_selective_step(x[:, :3].contiguous(), x[:, :3].contiguous(), A, B[:, :3].contiguous(), B[:, :3].contiguous(), D_, bias, h0,
+                                 y[:, :3].contiguous(), la.LA_STEP_SOFTPLUS)
+            out.append(h0)
+    if not hasattr(test_calls_in_native_code_and_in_python, "out"):
+        test_calls_in_native_code_and_in_python.out = out
+    for a, c in zip(out, test_calls_in_native_code_and_in_python.out):
+        assert (a is None) == (c is None) and (a is None or torch.equal(a, c))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_gradients_of_gradients_are_refused(monkeypatch, native):
+    la.load_library()
+    if not native:
+        monkeypatch.setattr(binding, "_native", None)
+    for name, (f, inputs) in calls(torch.float32).items():
+        ts = [t.clone().requires_grad_(True) for t in inputs]
+        out = f(*ts)[0]
+        first = torch.autograd.grad((out * out).sum(), ts[0], create_graph=True)[0]
+        with pytest.raises(RuntimeError):
+            torch.autograd.grad((first * first).sum(), ts[0])
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_refusals_in_the_same_words(monkeypatch, native):
+    la.load_library()
+    if not native:
+        monkeypatch.setattr(binding, "_native", None)
+    x, w, A, B, D = rand(4, 8, 16), rand(16, 4), rand(16, 5), rand(4, 8, 5), rand(16)
+    said = []
+    for bad in (lambda: la.causal_conv(x, w[:3]), lambda: la.causal_conv(x, w.half()), lambda: la.causal_conv(x, w, D[:2]), lambda: la.causal_conv(x, w, D, x),
+                lambda: la.causal_conv(x, w, lengths=D), lambda: la.causal_conv(x, w[:, :1]), lambda: la.causal_conv(x[:0], w), lambda: la.causal_conv(x.half(), w),
+                lambda: la.causal_conv(D, w), lambda: la.causal_conv(x, D), lambda: la.causal_conv(x, rand(16, 9)), lambda: la.causal_conv(x.cpu(), w),
+                lambda: la.selective_scan(x, x[:2], A, B, B), lambda: la.selective_scan(x, x, A[:3], B, B), lambda: la.selective_scan(x, x, A.half(), B, B),
+                lambda: la.selective_scan(x, x, A, B[..., :3], B), lambda: la.selective_scan(x, x, A, B, B[..., :3]),
+                lambda: la.selective_scan(x, x, A, B.bfloat16(), B), lambda: la.selective_scan(x, x, A, B, B, D[:3]),
+                lambda: la.selective_scan(x, x, A, B, B, D, None, D), lambda: la.selective_scan(x, x, A, B, B, lengths=D),
+                lambda: la.selective_scan(x, x, rand(16, 129), rand(4, 8, 129), rand(4, 8, 129)), lambda: la.selective_scan(x[:, :0], x[:, :0], A, B[:, :0], B[:, :0]),
+                lambda: la.selective_scan(x, x, A, rand(4, 8, 3, 5), rand(4, 8, 3, 5)), lambda: la.selective_scan(x, x, D, B, B)):
+        with pytest.raises((ValueError, TypeError, la.LaError)) as e:
+            bad()
+        said.append("%s: %s" % (type(e.value).__name__, e.value))
+    if not hasattr(test_refusals_in_the_same_words, "said"):
+        test_refusals_in_the_same_words.said = said
+    assert said == test_refusals_in_the_same_words.said
+
+
+def test_what_is_written_is_seen():
+    """A backward pass refuses where one of the tensors that it kept was written by a call since."""
+    x, w, st = rand(2, 9, 16).requires_grad_(True), rand(16, 4, seed=1), rand(2, 3, 16, seed=2)
+    y, _ = la.causal_conv(x, w, None, st)
+    la.la_conv_step(x.detach()[:, :1].contiguous(), w, None, st, torch.empty(2, 1, 16, device="cuda"), la.LA_ACT_SILU)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.sum().backward()
+    A, B, h0 = -torch.exp(rand(16, 8, seed=3)), rand(2, 9, 8, seed=4), rand(2, 16, 8, seed=5)
+    dt = rand(2, 9, 16, seed=6)
+    y, last = la.selective_scan(x, dt, A, B, B, h0=h0)
+    tokens = [x.detach()[:, :1].contiguous(), x.detach()[:, :1].contiguous(), A, B[:, :1].contiguous(), B[:, :1].contiguous()]
+    la.la_selective_step(*tokens, None, None, h0, torch.empty(2, 1, 16, device="cuda"), la.LA_STEP_VALUE)
+    torch.autograd.grad(y.sum(), x, retain_graph=True)  # h0 itself is not kept
+    la.la_selective_step(*tokens, None, None, h0, dt.view(1, 18, 16)[:, :2].view(2, 1, 16), la.LA_STEP_VALUE)
+    with pytest.raises(RuntimeError, match="modified by an inplace"):
+        y.sum().backward()
+
+
+def layer(x, w, b, proj, A, D, bias, n=None, state=(None, None)):
+    """The convolution, then the scan with B, C and dt from its output, as a layer runs them."""
+    u, rows = la.causal_conv(x, w, b, state[0], n)
+    v = u.float() @ proj
+    v = v.to(x.dtype)
+    C, S = A.shape
+    y, h = la.selective_scan(u, v[..., :C], A, v[..., C:C + S], v[..., C + S:], D, bias, state[1], n)
+    return y, rows, h
+
+
+def layer_inputs(k, dtype=torch.float32, B=2, N=200, C=96, S=16):
+    wide = rand(B, N, 2 * C, seed=20 * k, dtype=dtype)
+    return [wide, rand(C, 4, seed=20 * k + 1) / 2, rand(C, seed=20 * k + 2), rand(C, C + 2 * S, seed=20 * k + 3) / C ** 0.5,
+            -torch.exp(rand(C, S, seed=20 * k + 4)), rand(C, seed=20 * k + 5), rand(C, seed=20 * k + 6) - 3]
+
+
+def test_a_layer_against_64_bits():
+    """The run of the two, on a padded batch, against their definitions one behind the other."""
+    ins = layer_inputs(0)
+    n = torch.tensor([200, 77], dtype=torch.int32)
+    x = ins[0][..., 96:]
+    y, rows, h = layer(x, *ins[1:], n.cuda())
+    w, b, proj, A, D, bias = (t.cpu() for t in ins[1:])
+    u, _, _ = conv64(x.cpu(), w, b, None, n, "silu")
+    got_u, _ = la.causal_conv(x, ins[1], ins[2], None, n.cuda())
+    v = (got_u @ ins[3]).cpu()  # what the scan is given: its own bounds hold from there on
+    s = Scan64(got_u.cpu(), v[..., :96], A, v[..., 96:112].unsqueeze(2), v[..., 112:].unsqueeze(2), D, bias, None, n, "softplus")
+    within(y, s.y, s.Ey, torch.float32)
+    within(h, s.last, s.Elast, torch.float32)
+    assert (got_u.cpu().double() - u).abs().max() < 1e-5  # conv64's own test has the bound
+
+
+def test_a_prompt_and_tokens_of_a_layer():
+    """A prompt through the layer, then token by token from the carried rows and state: what the layer gives on all rows at
+    once, within the roundings of two orders of the same sums (2^-24 of terms of some units over a hundred rows)."""
+    ins = layer_inputs(1)
+    x = ins[0][..., :96]
+    want, rows, h = layer(x, *ins[1:])
+    y, st, state = layer(x[:, :150].contiguous(), *ins[1:])
+    parts = [y]
+    w, b, proj, A, D, bias = ins[1:]
+    for t in range(150, 200):
+        u, o = torch.empty(2, 1, 96, device="cuda"), torch.empty(2, 1, 96, device="cuda")
+        la.la_conv_step(x[:, t:t + 1], w, b, st, u, la.LA_ACT_SILU)
+        v = u @ proj
+        la.la_selective_step(u, v[..., :96], A, v[..., 96:112], v[..., 112:], D, bias, state, o, la.LA_STEP_SOFTPLUS)
+        parts.append(o)
+    assert torch.equal(st, rows)
+    got = torch.cat(parts, 1)
+    assert ((got - want).abs() <= 1e-4 * (1 + want.abs())).all() and ((state - h).abs() <= 1e-4 * (1 + h.abs())).all()
+
+
+def step_of(ins, dy):
+    y, rows, h = layer(ins[0][..., :96], *ins[1:])
+    return [y, rows, h, *torch.autograd.grad([y, h], ins, [dy, h.detach()])]
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_captured_training_step(dtype):
+    """Forward and backward of the layer in a graph, replayed on new inputs with eager steps in between; every replay gives the eager
+    step's bits."""
+    draw = lambda k: [t.requires_grad_(True) for t in layer_inputs(k, dtype)]  # noqa: E731
+    dy = rand(2, 200, 96, seed=99, dtype=dtype)
+    ins = draw(0)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step_of(ins, dy)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = step_of(ins, dy)
+    for k in (1, 2, 0, 1):
+        new = draw(k)
+        with torch.no_grad():
+            for a, b in zip(ins, new):
+                a.copy_(b)
+        want = step_of(new, dy)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(outs, want))
+
+
+def test_two_runs_give_the_same_bits():
+    for dtype in (torch.float32, torch.bfloat16):
+        ins = [t.requires_grad_(True) for t in layer_inputs(3, dtype, B=3, N=700)]
+        dy = rand(3, 700, 96, seed=98, dtype=dtype)
+        first, second = step_of(ins, dy), step_of(ins, dy)
+        assert all(torch.equal(a, b) for a, b in zip(first, second))
+
+
+def test_threads_with_streams_of_their_own():
+    """Four threads at once give the bits of calls that run alone."""
+    sets = [[t.requires_grad_(True) for t in layer_inputs(k)] for k in range(4)]
+    dy = rand(2, 200, 96, seed=97)
+    alone = [[t.detach() for t in step_of(s, dy)] for s in sets]
+    torch.cuda.synchronize()
+    bad = []
+
+    def work(k):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(10):
+                    got = step_of(sets[k], dy)
+                    torch.cuda.current_stream().synchronize()
+                    if not all(torch.equal(a, b) for a, b in zip(got, alone[k])):
+                        bad.append(k)
+        except Exception as e:
+            bad.append(e)
+    threads = [threading.Thread(target=work, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_calls_on_a_stream_given_by_name(monkeypatch, native):
+    """They run behind the work that is already there, and other streams that wait for it find their results."""
+    la.load_library()
+    if not native:
+        monkeypatch.setattr(binding, "_native", None)
+    ins = layer_inputs(5)
+    x, w, b, proj, A, D, bias = ins
+    x = x[..., :96].contiguous()
+    dt, Bm, h0 = rand(2, 200, 96, seed=50), rand(2, 200, 16, seed=51), rand(2, 96, 16, seed=52)
+    sources = [x, w, b, A, D, bias, dt, Bm, h0]
+
+    def outputs(stream, t):
+        x, w, b, A, D, bias, dt, Bm, h0 = t
+        e = torch.empty_like
+        y, z, dx, ddt, dx2, last, dw, db = e(x), e(x), e(x), e(x), e(x), torch.empty(2, 3, 96, device="cuda"), e(w), e(b)
+        dA, dB, dC, dD, dbias, dh0, h = e(A), e(Bm), e(Bm), e(D), e(bias), e(h0), e(h0)
+        U = dict(dtype=torch.uint8, device="cuda")
+        ws = torch.full((max(la.la_conv_workspace_bytes(2, 200, 96, 4), la.la_selective_workspace_bytes(2, 200, 96, 16, 1, 0),
+                             la.la_selective_workspace_bytes(2, 200, 96, 16, 1, 1)),), 0xFF, **U)
+        kept = torch.full((la.la_selective_saved_bytes(2, 200, 96, 16),), 0xFF, **U)
+        torch.cuda.current_stream().synchronize()
+        la.la_conv_forward(x, w, b, None, y, last, None, la.LA_ACT_SILU, stream=stream)
+        la.la_selective_forward(y, dt, A, Bm, Bm, D, bias, h0, z, h, kept, None, la.LA_STEP_SOFTPLUS, ws, stream=stream)
+        la.la_selective_backward(y, dt, A, Bm, Bm, D, bias, kept, z, h, dx, ddt, dA, dB, dC, dD, dbias, dh0, None, la.LA_STEP_SOFTPLUS, ws, stream=stream)
+        la.la_conv_backward(x, w, b, None, dx, last, dx2, dw, db, None, None, la.LA_ACT_SILU, ws, stream=stream)
+        return [y, last, z, h, dx, ddt, dA, dB, dC, dD, dbias, dh0, dx2, dw, db]
+    want = outputs(None, sources)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    late = [torch.zeros_like(t) for t in sources]
+    for turn in range(2):
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):  # the inputs arrive on that stream, behind a copy that takes its time
+            torch.empty(1 << 28, dtype=torch.uint8, device="cuda").fill_(turn)
+            for a, c in zip(late, sources):
+                a.copy_(c)
+        got = outputs(side, late)
+        torch.cuda.current_stream().wait_stream(side)
+        assert all(torch.equal(a, c) for a, c in zip(got, want))
+        for t in late:
+            t.zero_()
+    torch.cuda.synchronize()
