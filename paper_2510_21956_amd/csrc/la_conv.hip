@@ -1,6 +1,6 @@
 // Short causal convolution along the rows, one filter of W taps a channel, with an activation: forward, backward, in steps.
 //
-// A lane takes V neighbouring channels (16 bytes) down a run of rows and keeps the W - 1 rows before the current one in
+// A lane takes V neighbouring channels down a run of rows and keeps the W - 1 rows before the current one in
 // registers: every row is read once, but for the W - 1 rows in front of a run.  Rows may start at any element: the
 // lane at a row's end takes its last V channels once more.
 //
@@ -90,32 +90,36 @@ __device__ __forceinline__ Piece<T, V> row_at(const Conv &a, int b, int t, int c
     return Piece<T, V>{};
 }
 
-template <typename T, int V, int W, int ACT, typename WT>
+// What the activation is given, of rows that stand in a ring of W, the oldest at I % W.
+template <int I, typename WT, int V, int W>
 __device__ __forceinline__ Wide<V> before_act(const Taps<WT, V, W> &taps, const Wide<V> (&past)[W])
 {
     Wide<V> v = taps.bias;
 #pragma unroll
     for (int j = 0; j < W; ++j)
 #pragma unroll
-        for (int k = 0; k < V; ++k) v.x[k] = fmaf(taps.w[j].x[k], past[j].x[k], v.x[k]);
+        for (int k = 0; k < V; ++k) v.x[k] = fmaf(taps.w[j].x[k], past[(I + j) % W].x[k], v.x[k]);
     return v;
 }
+// Rows that a loop takes together: whole turns of the ring, four at least, and as many are asked for ahead.
+template <int W>
+constexpr int rows_together = W >= 4 ? W : W == 3 ? 6 : 4;
 
 // Items: (sequence, run of rows, V channels), then (sequence, carried row, V channels) where `last` is wanted.
 template <typename T, typename WT, int V, int W, int ACT>
 __global__ void __launch_bounds__(256) k_conv(Conv a)
 {
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    const int each = (a.C + V - 1) / V;
+    const int pieces = (a.C + V - 1) / V;
     if (i >= a.items) {
         const size_t k = i - a.items;
-        if (!a.last || k >= (size_t)a.B * (W - 1) * each) return;
-        const int c = min((int)(k % each) * V, a.C - V), j = (int)(k / each % (W - 1)), b = (int)(k / each / (W - 1));
+        if (!a.last || k >= (size_t)a.B * (W - 1) * pieces) return;
+        const int c = min((int)(k % pieces) * V, a.C - V), j = (int)(k / pieces % (W - 1)), b = (int)(k / pieces / (W - 1));
         const Piece<T, V> p = row_at<T, V, W>(a, b, rows_of(a, b) - (W - 1) + j, c);
         __builtin_memcpy((T *)a.last + ((size_t)b * (W - 1) + j) * a.C + c, &p, sizeof p);
         return;
     }
-    const int c = min((int)(i % each) * V, a.C - V), r = (int)(i / each % a.runs), b = (int)(i / each / a.runs);
+    const int c = min((int)(i % pieces) * V, a.C - V), r = (int)(i / pieces % a.runs), b = (int)(i / pieces / a.runs);
     const int n = rows_of(a, b), t0 = r * a.run, end = min(a.N, t0 + a.run), stop = min(n, end);
     T *Y = (T *)a.Y + ((size_t)b * a.N + t0) * a.C + c;
     int t = t0;
@@ -125,17 +129,17 @@ __global__ void __launch_bounds__(256) k_conv(Conv a)
 #pragma unroll
         for (int j = 0; j < W - 1; ++j) past[j] = widened(row_at<T, V, W>(a, b, t0 - (W - 1) + j, c));
         const T *X = (const T *)a.X + ((size_t)b * a.N + t0) * a.xs + c;
-        constexpr int AHEAD = 4;
-        Piece<T, V> next[AHEAD];
+        constexpr int U = rows_together<W>;
+        Piece<T, V> next[U];
 #pragma unroll
-        for (int k = 0; k < AHEAD; ++k) next[k] = fetch<T, V>(X + (size_t)min(k, stop - 1 - t0) * a.xs);
-        for (; t < stop; t += AHEAD)
-#pragma unroll
-            for (int k = 0; k < AHEAD; ++k) {
-                if (t + k >= stop) break;
-                past[W - 1] = widened(next[k]);
-                next[k] = fetch<T, V>(X + (size_t)(min(t + k + AHEAD, stop - 1) - t0) * a.xs);
-                Wide<V> v = before_act<T, V, W, ACT>(taps, past);
+        for (int k = 0; k < U; ++k) next[k] = fetch<T, V>(X + (size_t)min(k, stop - 1 - t0) * a.xs);
+        for (; t < stop; t += U)
+            each<U>([&](auto k_) {
+                constexpr int k = decltype(k_)::value;
+                if (t + k >= stop) return;
+                past[(k + W - 1) % W] = widened(next[k]);
+                next[k] = fetch<T, V>(X + (size_t)(min(t + k + U, stop - 1) - t0) * a.xs);
+                Wide<V> v = before_act<k>(taps, past);
                 if (ACT == LA_ACT_SILU)
 #pragma unroll
                     for (int m = 0; m < V; ++m) {
@@ -145,9 +149,7 @@ __global__ void __launch_bounds__(256) k_conv(Conv a)
                     }
                 put<T, V>(Y, v);
                 Y += a.C;
-#pragma unroll
-                for (int j = 0; j < W - 1; ++j) past[j] = past[j + 1];
-            }
+            });
         t = stop;
     }
     for (; t < end; ++t) {
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(256) k_conv_back(Conv a)
         const size_t row0 = (size_t)b * a.N;
         const Taps<WT, V, W> taps(a, c);
         const int own = min(n, end), stop = min(n, end + W - 1);  // e of rows [t0, stop)
-        // e_t for the last W rows, newest last; x for the last W
+        // e and x of the last W rows, in rings
         Wide<V> e[W], past[W];
 #pragma unroll
         for (int j = 0; j < W; ++j) e[j] = Wide<V>{};
@@ -185,57 +187,76 @@ __global__ void __launch_bounds__(256) k_conv_back(Conv a)
             for (int j = 0; j < W - 1; ++j) past[j] = widened(row_at<T, V, W>(a, b, t0 - (W - 1) + j, c));
         const T *X = (const T *)a.X + row0 * a.xs + c, *dY = (const T *)a.dY + row0 * a.C + c;
         T *dX = (T *)a.dX + row0 * a.C + c;
-        Piece<T, V> nx{}, ny{};
-        if (t0 < stop) nx = fetch<T, V>(X + (size_t)t0 * a.xs), ny = fetch<T, V>(dY + (size_t)t0 * a.C);
+        constexpr int U = rows_together<W>;
+        Piece<T, V> nx[U], ny[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            if (t0 < stop) {
+                const int m = min(t0 + k, stop - 1);
+                nx[k] = fetch<T, V>(X + (size_t)m * a.xs), ny[k] = fetch<T, V>(dY + (size_t)m * a.C);
+            }
         // dx of row s = t - (W - 1) is complete once e_t is there; rows before the first are the carried ones
-        for (int t = t0; t < end + W - 1; ++t) {
+        const int from = n - (W - 1);  // the first row that is carried on
+        const T *Xt = X + (size_t)(t0 + U) * a.xs, *dYt = dY + (size_t)(t0 + U) * a.C;  // rows asked for next
+        T *dXt = dX + (ptrdiff_t)(t0 - (W - 1)) * a.C;
+        // PLAIN: all rows of the turn are the run's own, and so is what they complete and ask for
+        auto turn = [&](int t1, auto plain_) {
+            constexpr bool PLAIN = decltype(plain_)::value;
+            each<U>([&](auto k_) {
+                constexpr int k = decltype(k_)::value, now = (k + W - 1) % W;
+                const int t = t1 + k;
+                if (!PLAIN && t >= end + W - 1) return;
+                if (!PLAIN) e[now] = Wide<V>{};
+                if (PLAIN || t < stop) {
+                    past[now] = widened(nx[k]);
+                    Wide<V> g = widened(ny[k]);
+                    if (PLAIN) nx[k] = fetch<T, V>(Xt), ny[k] = fetch<T, V>(dYt);
+                    else {
+                        const int m = min(t + U, stop - 1);
+                        nx[k] = fetch<T, V>(X + (size_t)m * a.xs), ny[k] = fetch<T, V>(dY + (size_t)m * a.C);
+                    }
+                    if (ACT == LA_ACT_SILU) {
+                        const Wide<V> v = before_act<k>(taps, past);
 #pragma unroll
-            for (int j = 0; j < W - 1; ++j) e[j] = e[j + 1];
-            if (t < stop) {
-                past[W - 1] = widened(nx);
-                Wide<V> g = widened(ny);
-                const int m = min(t + 1, stop - 1);
-                nx = fetch<T, V>(X + (size_t)m * a.xs), ny = fetch<T, V>(dY + (size_t)m * a.C);
-                if (ACT == LA_ACT_SILU) {
-                    const Wide<V> v = before_act<T, V, W, ACT>(taps, past);
+                        for (int q = 0; q < V; ++q) {
+                            float f, rest;
+                            sigmoid<sizeof(T) == 4>(v.x[q], f, rest);
+                            g.x[q] *= f * fmaf(v.x[q], rest, 1.f);
+                        }
+                    }
+                    e[now] = g;
+                    if (PLAIN || t < own) {
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        float f, rest;
-                        sigmoid<sizeof(T) == 4>(v.x[k], f, rest);
-                        g.x[k] *= f * fmaf(v.x[k], rest, 1.f);
+                        for (int q = 0; q < V; ++q) {
+                            db.x[q] += g.x[q];
+#pragma unroll
+                            for (int j = 0; j < W; ++j) dw[j].x[q] = fmaf(g.x[q], past[(k + j) % W].x[q], dw[j].x[q]);
+                        }
                     }
                 }
-                e[W - 1] = g;
-                if (t < own) {
+                T *const to = dXt;
+                Xt += a.xs, dYt += a.C, dXt += a.C;
+                const int s = t - (W - 1);
+                if (!PLAIN && s < t0 && (t0 > 0 || !a.dstate)) return;
+                // e of row s + j is in place (k + j) % W
+                Wide<V> d{};
 #pragma unroll
-                    for (int k = 0; k < V; ++k) {
-                        db.x[k] += g.x[k];
+                for (int j = 0; j < W; ++j)
 #pragma unroll
-                        for (int j = 0; j < W; ++j) dw[j].x[k] = fmaf(g.x[k], past[j].x[k], dw[j].x[k]);
-                    }
+                    for (int q = 0; q < V; ++q) d.x[q] = fmaf(taps.w[W - 1 - j].x[q], e[(k + j) % W].x[q], d.x[q]);
+                if (!PLAIN && a.dlast && s >= from && s < n) {
+                    const Wide<V> l = widened(fetch<T, V>((const T *)a.dlast + ((size_t)b * (W - 1) + s - from) * a.C + c));
+#pragma unroll
+                    for (int q = 0; q < V; ++q) d.x[q] += l.x[q];
                 }
-#pragma unroll
-                for (int j = 0; j < W - 1; ++j) past[j] = past[j + 1];
-            } else {
-                e[W - 1] = Wide<V>{};
-            }
-            const int s = t - (W - 1);
-            if (s < t0 && (t0 > 0 || !a.dstate)) continue;
-            // e[k] is e of row s + k
-            Wide<V> d{};
-#pragma unroll
-            for (int k = 0; k < W; ++k)
-#pragma unroll
-                for (int m = 0; m < V; ++m) d.x[m] = fmaf(taps.w[W - 1 - k].x[m], e[k].x[m], d.x[m]);
-            // the rows carried on are n - (W - 1) .. n - 1
-            const int from = n - (W - 1);
-            if (a.dlast && s >= from && s < n) {
-                const Wide<V> l = widened(fetch<T, V>((const T *)a.dlast + ((size_t)b * (W - 1) + s - from) * a.C + c));
-#pragma unroll
-                for (int m = 0; m < V; ++m) d.x[m] += l.x[m];
-            }
-            if (s >= 0) put<T, V>(dX + (size_t)s * a.C, d);
-            else put<T, V>((T *)a.dstate + ((size_t)b * (W - 1) + s + W - 1) * a.C + c, d);
+                if (PLAIN || s >= 0) put<T, V>(to, d);
+                else put<T, V>((T *)a.dstate + ((size_t)b * (W - 1) + s + W - 1) * a.C + c, d);
+            });
+        };
+        const int plain = min(own, min(stop - U, from + W - 1));  // up to where
+        for (int t1 = t0; t1 < end + W - 1; t1 += U) {
+            if (__all(t1 >= t0 + W - 1 && t1 + U <= plain)) turn(t1, std::true_type());
+            else turn(t1, std::false_type());
         }
     }
     if (!a.shares) return;
@@ -317,9 +338,12 @@ __global__ void __launch_bounds__(256) k_conv_step(Conv a)
 
 constexpr int kMostTaps = 8;
 
-// Channels a lane takes: 16 bytes of them; half as many where the taps would fill the registers; one where a row is shorter.
-template <typename T, int W>
-constexpr int wide_of = (sizeof(T) == 4 ? 4 : 8) / (W > 4 ? 2 : 1);
+// Channels a lane takes: four, two where the taps would fill the registers, backward two; one where a row is shorter.  More of
+// them leave fewer waves, whose loads are not enough: 8 x 2048 rows of 2048, bf16, forward 29 us, with eight 36; backward
+// 58, with four 59 and with eight 76.
+template <int W>
+constexpr int wide_of = W > 4 ? 2 : 4;
+constexpr int kWideBack = 2;
 
 // Rows of a run: enough waves to fill the chip, and few rows read twice.
 int run_rows(int B, int N, size_t pieces)
@@ -389,12 +413,7 @@ extern "C" {
 size_t la_conv_workspace_bytes(int B, int N, int C, int W)
 {
     if (la::check(C < 1 ? 1 : C, B, N, C, W, LA_ACT_NONE, LA_F32, LA_F32) != LA_OK) return 0;
-    size_t most = 0;  // of either type
-    for (int V : {W > 4 ? 2 : 4, W > 4 ? 4 : 8}) {
-        const size_t n = (size_t)la::back_of(B, N, C, V).count;
-        most = n > most ? n : most;
-    }
-    return la::round_up(most * (W + 1) * C * 4, 256);
+    return la::round_up((size_t)la::back_of(B, N, C, la::kWideBack).count * (W + 1) * C * 4, 256);
 }
 
 la_status la_conv_forward(const void *X, size_t x_stride, const void *Wt, const void *bias, const void *state, void *Y, void *last,
@@ -417,7 +436,7 @@ la_status la_conv_forward(const void *X, size_t x_stride, const void *Wt, const 
     la::by_kind(dt, wt, act, W, [&](auto *t, auto *w, auto act_, auto taps) {
         typedef std::remove_pointer_t<decltype(t)> T;
         typedef std::remove_pointer_t<decltype(w)> WT;
-        constexpr int K = decltype(taps)::value, V = la::wide_of<T, K>;
+        constexpr int K = decltype(taps)::value, V = la::wide_of<K>;
         auto go = [&](auto wide) {
             constexpr int U = decltype(wide)::value;
             const size_t each = (C + U - 1) / U;
@@ -461,7 +480,7 @@ la_status la_conv_backward(const void *X, size_t x_stride, const void *Wt, const
     la::by_kind(dt, wt, act, W, [&](auto *t, auto *w, auto act_, auto taps) {
         typedef std::remove_pointer_t<decltype(t)> T;
         typedef std::remove_pointer_t<decltype(w)> WT;
-        constexpr int K = decltype(taps)::value, V = la::wide_of<T, K>;
+        constexpr int K = decltype(taps)::value, V = la::kWideBack;
         const la::Back p = la::back_of(B, N, C, V);
         a.lanes = p.lanes, a.columns = p.columns, a.run = p.run, a.runs = p.runs;
         auto go = [&](auto wide) {

@@ -1,5 +1,7 @@
-// Scalar functions of the operators around the attention.
+// Scalar functions of the operators around the attention, and a loop over constants.
 #pragma once
+
+#include <type_traits>
 
 #include "la_common.h"
 
@@ -45,6 +47,16 @@ __device__ __forceinline__ float softplus_of(float x, float E)
     p = fmaf(z, p, 2.f / 3.f);
     p = fmaf(z, p, 2.f);
     return fmaf(s, p, fmaxf(x, 0.f));
+}
+
+// f(0), f(1), .. as constants.
+template <int N, int I = 0, typename F>
+__device__ __forceinline__ void each(F f)
+{
+    if constexpr (I < N) {
+        f(std::integral_constant<int, I>());
+        each<N, I + 1>(f);
+    }
 }
 
 }  // namespace la

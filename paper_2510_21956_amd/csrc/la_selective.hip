@@ -112,16 +112,6 @@ __device__ __forceinline__ void keep_order()
 // x is there here, and not where it is used: what it was made from is let go of.
 __device__ __forceinline__ void settle(float &x) { asm volatile("" : "+v"(x)); }
 
-// f(0), f(1), .. as constants.
-template <int N, int I = 0, typename F>
-__device__ __forceinline__ void each(F f)
-{
-    if constexpr (I < N) {
-        f(std::integral_constant<int, I>());
-        each<N, I + 1>(f);
-    }
-}
-
 // B or C of a tile for the P states of a wave: value P row + state stands in lane (P row + state) % 16 of every 16 lanes of a
 // register, from where the instruction that needs it reads it for all of them; zeros behind the last state and row.
 template <typename T, int P>
@@ -168,24 +158,42 @@ __device__ __forceinline__ float of_lane(float v)
 {
     return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), 0x150 + K, 0xf, 0xf, true));
 }
-// acc_j += v_{K+j} x, and acc += sum_j v_{K+j} x_j, v_k being the value of lane k of 16.  (A register that another lane's value is
-// read from is ready two instructions after it was written.)
-#define LA_FMA_OF_LANE(acc, x, k) "v_fmac_f32_dpp " acc ", %[v], " x " row_newbcast:" k " row_mask:0xf bank_mask:0xf\n\t"
+// acc_j += v_{K+j} x, and sum_j v_{K+j} x_j, v_k being the value of lane k of 16.  (A register that another lane's value is read
+// from is ready two instructions after it was written.)
+#define LA_OF_LANE(op, acc, x, k) "v_" op "_f32_dpp " acc ", %[v], " x " row_newbcast:" k " row_mask:0xf bank_mask:0xf\n\t"
 template <int K, int P, int J = 0>
 __device__ __forceinline__ void fma_each(float (&acc)[P], float v, float x)
 {
-    asm("s_nop 1\n\t" LA_FMA_OF_LANE("%0", "%[x]", "%[k0]") LA_FMA_OF_LANE("%1", "%[x]", "%[k1]")
-        : "+v"(acc[J]), "+v"(acc[J + 1]) : [v] "v"(v), [x] "v"(x), [k0] "n"(K + J), [k1] "n"(K + J + 1));
-    if constexpr (J + 2 < P) fma_each<K, P, J + 2>(acc, v, x);
+    if constexpr (P == 2)
+        asm("s_nop 1\n\t" LA_OF_LANE("fmac", "%0", "%[x]", "%[k0]") LA_OF_LANE("fmac", "%1", "%[x]", "%[k1]")
+            : "+v"(acc[0]), "+v"(acc[1]) : [v] "v"(v), [x] "v"(x), [k0] "n"(K), [k1] "n"(K + 1));
+    else {
+        asm("s_nop 1\n\t" LA_OF_LANE("fmac", "%0", "%[x]", "%[k0]") LA_OF_LANE("fmac", "%1", "%[x]", "%[k1]")
+            LA_OF_LANE("fmac", "%2", "%[x]", "%[k2]") LA_OF_LANE("fmac", "%3", "%[x]", "%[k3]")
+            : "+v"(acc[J]), "+v"(acc[J + 1]), "+v"(acc[J + 2]), "+v"(acc[J + 3])
+            : [v] "v"(v), [x] "v"(x), [k0] "n"(K + J), [k1] "n"(K + J + 1), [k2] "n"(K + J + 2), [k3] "n"(K + J + 3));
+        if constexpr (J + 4 < P) fma_each<K, P, J + 4>(acc, v, x);
+    }
 }
 template <int K, int P, int J = 0>
-__device__ __forceinline__ void fma_all(float &acc, float v, const float (&x)[P])
+__device__ __forceinline__ float sum_all(float v, const float (&x)[P])
 {
-    asm("s_nop 1\n\t" LA_FMA_OF_LANE("%0", "%[x0]", "%[k0]") LA_FMA_OF_LANE("%0", "%[x1]", "%[k1]")
-        : "+v"(acc) : [v] "v"(v), [x0] "v"(x[J]), [x1] "v"(x[J + 1]), [k0] "n"(K + J), [k1] "n"(K + J + 1));
-    if constexpr (J + 2 < P) fma_all<K, P, J + 2>(acc, v, x);
+    float a, b = 0.f;
+    if constexpr (P == 2)
+        asm("s_nop 1\n\t" LA_OF_LANE("mul", "%0", "%[x0]", "%[k0]") LA_OF_LANE("fmac", "%0", "%[x1]", "%[k1]")
+            : "=&v"(a) : [v] "v"(v), [x0] "v"(x[0]), [x1] "v"(x[1]), [k0] "n"(K), [k1] "n"(K + 1));
+    else {
+        asm("s_nop 1\n\t" LA_OF_LANE("mul", "%0", "%[x0]", "%[k0]") LA_OF_LANE("mul", "%1", "%[x1]", "%[k1]")
+            LA_OF_LANE("fmac", "%0", "%[x2]", "%[k2]") LA_OF_LANE("fmac", "%1", "%[x3]", "%[k3]")
+            : "=&v"(a), "=&v"(b)
+            : [v] "v"(v), [x0] "v"(x[J]), [x1] "v"(x[J + 1]), [x2] "v"(x[J + 2]), [x3] "v"(x[J + 3]), [k0] "n"(K + J), [k1] "n"(K + J + 1),
+              [k2] "n"(K + J + 2), [k3] "n"(K + J + 3));
+        a += b;
+        if constexpr (J + 4 < P) a += sum_all<K, P, J + 4>(v, x);
+    }
+    return a;
 }
-#undef LA_FMA_OF_LANE
+#undef LA_OF_LANE
 
 template <int P>
 __device__ __forceinline__ void decays(const Scan &a, const Spot &p, int wave, float (&A)[P])
@@ -335,14 +343,14 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
         each<kPairs>([&](auto q_) {
             constexpr int q = decltype(q_)::value;
             const float4 after = du[q + 2 < kPairs ? q + 2 : kPairs - 1][lane];
-            float y[2] = {0.f, 0.f};
+            float y[2];
             if constexpr (q + 1 < kPairs) open(g, next);
             each<2>([&](auto r_) {
                 constexpr int r = decltype(r_)::value, k = (2 * q + r) * P;
                 each<P>([&](auto j) {
                     h[j] = fmaf(f[r * P + j], h[j], (r ? s.w : s.y) * of_lane<k % 16 + decltype(j)::value>(B.v[k / 16]));
                 });
-                if (FULL) fma_all<k % 16>(y[r], C.v[k / 16], h);
+                if (FULL) y[r] = sum_all<k % 16>(C.v[k / 16], h);
                 else span += r ? s.z : s.x;
             });
             if (FULL) ys[wave][q][lane] = make_float2(y[0], y[1]);
@@ -385,18 +393,22 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
 // the instruction's mask of banks; then halves and quarters of the wave change places, one instruction for two values; the
 // last four values are added up over four neighbours.  Lane l ends with values 32 l3 + 16 l2 + 8 l5 + 4 l4 + (0 .. 3), l3 being bit 3
 // of l.  An instruction that reads another lane's register needs two others behind the one that wrote it.
+#define LA_FOLD(to, from, how, banks) "v_add_f32_dpp " to ", " to ", " to " " how " row_mask:0xf bank_mask:0xf\n\t" \
+                                     "v_add_f32_dpp " to ", " from ", " from " " how " row_mask:0xf bank_mask:" banks "\n\t"
 __device__ __forceinline__ float4 over_lanes(float (&v)[64])
 {
 #pragma unroll
-    for (int i = 0; i < 32; ++i)
-        asm("s_nop 1\n\tv_add_f32_dpp %0, %1, %1 row_ror:8 row_mask:0xf bank_mask:0xf\n\t"
-            "v_add_f32_dpp %0, %2, %2 row_ror:8 row_mask:0xf bank_mask:0xc"
-            : "=&v"(v[i]) : "v"(v[i]), "v"(v[i + 32]));
+    for (int i = 0; i < 32; i += 4)
+        asm("s_nop 1\n\t" LA_FOLD("%0", "%4", "row_ror:8", "0xc") LA_FOLD("%1", "%5", "row_ror:8", "0xc")
+            LA_FOLD("%2", "%6", "row_ror:8", "0xc") LA_FOLD("%3", "%7", "row_ror:8", "0xc")
+            : "+v"(v[i]), "+v"(v[i + 1]), "+v"(v[i + 2]), "+v"(v[i + 3])
+            : "v"(v[i + 32]), "v"(v[i + 33]), "v"(v[i + 34]), "v"(v[i + 35]));
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
-        asm("s_nop 1\n\tv_add_f32_dpp %0, %1, %1 row_half_mirror row_mask:0xf bank_mask:0xf\n\t"
-            "v_add_f32_dpp %0, %2, %2 row_half_mirror row_mask:0xf bank_mask:0xa"
-            : "=&v"(v[i]) : "v"(v[i]), "v"(v[i + 16]));
+    for (int i = 0; i < 16; i += 4)
+        asm("s_nop 1\n\t" LA_FOLD("%0", "%4", "row_half_mirror", "0xa") LA_FOLD("%1", "%5", "row_half_mirror", "0xa")
+            LA_FOLD("%2", "%6", "row_half_mirror", "0xa") LA_FOLD("%3", "%7", "row_half_mirror", "0xa")
+            : "+v"(v[i]), "+v"(v[i + 1]), "+v"(v[i + 2]), "+v"(v[i + 3])
+            : "v"(v[i + 16]), "v"(v[i + 17]), "v"(v[i + 18]), "v"(v[i + 19]));
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 8]), false, false);
@@ -411,6 +423,7 @@ __device__ __forceinline__ float4 over_lanes(float (&v)[64])
     }
     return make_float4(v[0], v[1], v[2], v[3]);
 }
+#undef LA_FOLD
 
 // Backward.  FULL: outputs, walking the tiles from the far end: states from the saved ones before the tile on, then the rows in
 // reverse.  Else what the segment hands to the rows before it from nothing behind it.
@@ -523,25 +536,25 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(FUL
                     constexpr int q = PART / 2 - 1 - decltype(q_)::value;
                     const float4 next = du[first + (q ? q - 1 : q)][lane];
                     const float2 nexty = dys[first + (q ? q - 1 : q)][lane];
-                    float gu[2] = {0.f, 0.f}, gd[2] = {0.f, 0.f};
+                    float gu[2], gd[2];
                     each<2>([&](auto r_) {
                         constexpr int r = 1 - decltype(r_)::value, k = (2 * q + r) * P, at = k + 2 * first * P;
                         const float d = r ? s.z : s.x, u = r ? s.w : s.y, y = r ? y2.y : y2.x;
                         fma_each<at % 16>(carry, C.v[at / 16], y);
-                        fma_all<at % 16>(gu[r], B.v[at / 16], carry);
+                        gu[r] = sum_all<at % 16>(B.v[at / 16], carry);
 #pragma unroll
                         for (int j = 0; j < P; ++j) {
                             const float g = carry[j];
                             carry[j] = g * f[k + j];
                             const float e = carry[j] * (k ? h[k - P + j] : h0[j]);
-                            gd[r] = fmaf(e, A[j], gd[r]);
+                            gd[r] = j ? fmaf(e, A[j], gd[r]) : e * A[j];
                             own[j] = fmaf(e, d, own[j]);
                             f[k + j] = g * u;
                             h[k + j] *= y;
                             settle(f[k + j]), settle(h[k + j]), settle(own[j]), settle(carry[j]);
                         }
                     });
-                    gs[wave][first + q][lane] = make_float4(gu[0], gd[0] * kLn2, gu[1], gd[1] * kLn2);
+                    gs[wave][first + q][lane] = make_float4(gu[0], gd[0], gu[1], gd[1]);
                     s = next, y2 = nexty;
                     keep_order();
                 });
@@ -584,7 +597,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(FUL
 #pragma unroll
                 for (int r = 0; r < 2; ++r) {
                     const float gu = r ? g.z : g.x, gd = r ? g.w : g.y, y = r ? y2.y : y2.x;
-                    const float dd = fmaf(xw[i][r], gu, gd) * slope[i][r];
+                    const float dd = fmaf(xw[i][r], gu, gd * kLn2) * slope[i][r];
                     if (p.live && 2 * q + r < rows) {
                         dX.put(2 * q + r, fmaf(r ? s.z : s.x, gu, D * y));
                         dDt.put(2 * q + r, dd);
