@@ -584,15 +584,16 @@ LA_API la_status la_conv_step(const void *X, size_t x_stride, const void *Wt, co
  *       D, bias: [C] float32, or NULL for zeros.  dA, dD, dbias: their gradients, float32, or NULL where they are not wanted.
  *   h0, last, dlast, dh0: [B, C, S] float32.  h0 NULL: zeros; last (the state after the last row) NULL: not wanted; dlast NULL:
  *       zeros; dh0 NULL: not wanted.
- *   saved: states that the forward call leaves for the backward call, la_selective_saved_bytes(B, N, C, S) bytes, 256-byte aligned;
- *       NULL in a forward call that no backward call follows.  Its layout is private to the library.
+ *   saved: states that the forward call leaves for the backward call with the same arguments, those before every 16th row,
+ *       la_selective_saved_bytes(B, N, C, S) bytes (S / 4 for every element of X), 256-byte aligned; NULL in a forward call that no
+ *       backward call follows.  Its layout is private to the library.
  *   lengths: NULL, or B ints on the device.  Rows from lengths[b] on are padding: they are not read, every output is zero there, and
  *       `last` is the state before them (a length of 0 or less leaves h0, one of N or more is N).
  *   workspace: at least la_selective_workspace_bytes(B, N, C, S, G, is_backward) bytes, 256-byte aligned; NULL where that is 0.
  *       Nothing in it has to start at zero.  Calls that share one must not overlap in time, two captured graphs' neither.
  * States, products and sums are float32, the sums in a fixed order: two runs give the same bits.  Addresses are those of elements.
- * Limits: B, N, C, S, G >= 1, N <= 2^30, S <= 128, C a multiple of G, B * N * stride < 2^40 for every tensor,
- * B * G * ceil(C / G / 64) * ceil(N / 16) < 2^31 and, without the last factor, < 2^21.
+ * Limits: B, N, C, S, G >= 1, N <= 2^30, S <= 128, C a multiple of G, every stride, C and G * S < 2^24, B * N * stride < 2^40
+ * for every tensor, B * G * ceil(C / G / 64) * ceil(N / 16) < 2^31 and, without the last factor, < 2^21.
  *
  * la_selective_step appends T rows to a carried state, [B, C, S] float32, and updates it in place: the form for single
  * tokens.  No workspace; rows are walked one after another, T is meant to be small.  Calls that share a state must not overlap in time.

@@ -650,28 +650,52 @@ __global__ void __launch_bounds__(256) k_selective_shares(Scan a, T *dB, T *dC, 
         if (t >= a.N || s >= a.S) continue;
         const int n = a.lengths ? min(max(a.lengths[b], 0), a.N) : a.N;
         float sum = 0.f;
-        if (t < n)
-            for (int c = 0; c < a.per; ++c) sum += a.shares[(((size_t)b * a.columns + g * a.per + c) * a.tiles + tile) * each + v];
+        if (t < n) {
+            const size_t step = (size_t)a.tiles * each;
+            const float *from = a.shares + ((size_t)b * a.columns + g * a.per) * step + (size_t)tile * each + v;
+            int c = 0;
+            for (; c + 8 <= a.per; c += 8, from += 8 * step) {  // asked for together, added in order
+                float x[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) x[k] = from[k * step];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) sum += x[k];
+            }
+            for (; c < a.per; ++c, from += step) sum += *from;
+        }
         store_elem(v % 64 < kCells ? dB : dC, (((size_t)b * a.N + t) * a.G + g) * a.S + s, sum);
     }
 }
 
-// dA, dD and dbias from the segments' sums: 64 channels and one row of the sums a workgroup, its waves take every 4th
-// segment each.
-__global__ void __launch_bounds__(256) k_selective_join(Scan a, float *dA, float *dD, float *db)
+// dA, dD and dbias from the segments' sums: 64 channels and one row of the sums a workgroup, its waves take every 16th
+// segment each, eight of them asked for together.
+__global__ void __launch_bounds__(1024) k_selective_join(Scan a, float *dA, float *dD, float *db)
 {
-    __shared__ float sums[4][64];
+    __shared__ float sums[16][64];
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane, s = blockIdx.y;
     const int rows = s < a.S ? a.S : 2;
     const float *from = s < a.S ? a.dA + (size_t)s * a.C : a.dd + (size_t)(s - a.S) * a.C;
     if (s < a.S && !dA) return;
     float sum = 0.f;
-    if (c < a.C)
-        for (int k = wave; k < a.B * a.segs; k += 4) sum += from[(size_t)k * rows * a.C + c];
+    if (c < a.C) {
+        const int count = a.B * a.segs;
+        const size_t step = (size_t)rows * a.C;
+        int k = wave;
+        for (; k + 7 * 16 < count; k += 8 * 16) {
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = from[(size_t)(k + 16 * i) * step + c];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum += x[i];
+        }
+        for (; k < count; k += 16) sum += from[(size_t)k * step + c];
+    }
     sums[wave][lane] = sum;
     block_sync();
     if (wave || c >= a.C) return;
-    sum = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+    sum = 0.f;
+#pragma unroll
+    for (int k = 0; k < 16; ++k) sum += sums[k][lane];
     if (s < a.S) dA[(size_t)c * a.S + s] = sum;
     else if (s == a.S) {
         if (dD) dD[c] = sum;
@@ -765,7 +789,7 @@ la_status check(const Scan &a, la_step step, la_dtype dt)
     const size_t vec = (size_t)a.G * a.S;
     if (a.xs < (size_t)a.C || a.ts < (size_t)a.C || a.bs < vec || a.cs < vec) return LA_ERR_SHAPE;
     for (size_t n : {a.xs, a.ts, a.bs, a.cs, vec, (size_t)a.C})
-        if (n >= 1 << 24) return LA_ERR_SHAPE;  // rows of a tile in 32 bits
+        if (n >= 1 << 24) return LA_ERR_SHAPE;  // a tile's rows in 32 bits
     for (size_t n : {a.xs, a.ts, a.bs, a.cs, vec})
         if ((double)a.B * a.N * (double)n >= 1099511627776.0) return LA_ERR_SHAPE;  // 2^40
     if (!real_type(dt) || (step != LA_STEP_VALUE && step != LA_STEP_SOFTPLUS)) return LA_ERR_UNSUPPORTED;
@@ -792,7 +816,7 @@ struct Inputs {
 // How a call is laid out: the states of a wave, and the segments that sequences are cut into, whose start states two more launches
 // find (what every segment makes of zero states, an exponential and three operations for every row and state once more, and
 // the walk along the segments).  512 rows take, in us, with w waves on every SIMD of the busiest compute units (S = 16, bf16):
-// 39 + 29 w forward, 100 + 80 w backward, what the segments make of zero states 28 + 23 w and 31 + 21 w.  Segments fill the
+// 39 + 29 w forward (31 + 35 w with two states a wave), 100 + 80 w backward, what the segments make of zero states 28 + 23 w and 31 + 21 w.  Segments fill the
 // compute units once forward, about twice backward (5 and 3 or 4 waves to a SIMD at once), and have 32 rows at least; one
 // piece where that takes less.  Of 1 to 96 segments, on 10 shapes of 1 to 256 chains, this takes 1.04 times the best on the average.
 // Forward, one piece and few waves: two states a wave instead of four, whose twice as many waves hide each other's
@@ -811,13 +835,14 @@ Shape lay_out(Scan &a, bool backward)
     int segs = (int)(most < 256.0 ? most : 256.0);
     if (segs > a.N / 32) segs = a.N / 32;
     const double busiest = (double)(int)((chains + 255) / 256) * s.W / 4.0;
-    const double whole = rows * (backward ? 100 + 80 * busiest : 39 + 29 * busiest);
+    const bool two = !backward && a.S <= 16 && 31 + 35 * busiest < 39 + 29 * busiest;
+    const double whole = rows * (backward ? 100 + 80 * busiest : two ? 31 + 35 * busiest : 39 + 29 * busiest);
     const double cut = 8.0 + rows * (backward ? 101 * waves + 131.0 / segs : 52 * waves + 67.0 / segs);
     if (segs < 2 || whole <= cut) segs = 1;
     const int of = (a.tiles + segs - 1) / segs;
     a.seg = of * kRows;
     a.segs = (a.tiles + of - 1) / of;
-    return shape_of(a.S, !backward && a.segs == 1 && waves < 2.0);
+    return shape_of(a.S, two && a.segs == 1);
 }
 Scan scan_of(const void *X, size_t xs, const void *Dt, size_t ts, const float *A, const void *Bm, size_t bs, const void *Cm, size_t cs,
              const float *D, const float *bias, int B, int N, int C, int S, int G, la_step step)
@@ -975,7 +1000,7 @@ la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, 
     const dim3 all = la::blocks_of((size_t)B * G * a.tiles * la::shares_of(shape));
     if (dt == LA_F32) la::k_selective_shares<float><<<all, dim3(256), 0, st>>>(a, (float *)dBm, (float *)dCm, shape.P, shape.W);
     else la::k_selective_shares<la::bf16_t><<<all, dim3(256), 0, st>>>(a, (la::bf16_t *)dBm, (la::bf16_t *)dCm, shape.P, shape.W);
-    if (dA || dD || dbias) la::k_selective_join<<<dim3((C + 63) / 64, S + 2), dim3(256), 0, st>>>(a, dA, dD, dbias);
+    if (dA || dD || dbias) la::k_selective_join<<<dim3((C + 63) / 64, S + 2), dim3(1024), 0, st>>>(a, dA, dD, dbias);
     return la::done();
 }
 

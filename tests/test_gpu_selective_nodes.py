@@ -327,3 +327,47 @@ def test_calls_on_a_stream_given_by_name(monkeypatch, native):
         for t in late:
             t.zero_()
     torch.cuda.synchronize()
+
+
+def test_beyond_32_bits():
+    """More than 2^31 elements: the last rows, which lie behind it, as a call on them alone gives them."""
+    N, C = 1_050_000, 2048
+    assert N * C > 1 << 31
+    block = rand(1, 1050, C, dtype=torch.bfloat16)
+    x = block.repeat(1, 1000, 1)
+    w, b = rand(C, 4, seed=1), rand(C, seed=2)
+    y, last = la.causal_conv(x, w, b)
+    z, _ = la.causal_conv(x[:, -100:].contiguous(), w, b, state=x[:, -103:-100].contiguous())
+    assert torch.equal(y[:, -100:], z) and torch.equal(last, x[:, -3:])
+    # backward: the gradient of the last rows alone, and sums over rows that a gradient of zero elsewhere leaves to them
+    dy = torch.zeros_like(x)
+    dy[:, -50:] = rand(1, 50, C, seed=3, dtype=torch.bfloat16)
+    dx, dw, db = torch.empty_like(x), torch.empty_like(w), torch.empty_like(b)
+    ws = torch.empty(la.la_conv_workspace_bytes(1, N, C, 4), dtype=torch.uint8, device="cuda")
+    la.la_conv_backward(x, w, b, None, dy, None, dx, dw, db, None, None, la.LA_ACT_SILU, ws)
+    leaf = [t.requires_grad_(True) for t in (x[:, -100:].contiguous(), w.clone(), b.clone())]
+    o, _ = la.causal_conv(*leaf, state=x[:, -103:-100].contiguous())
+    gx, gw, gb = torch.autograd.grad(o, leaf, dy[:, -100:])
+    assert torch.equal(dx[:, -100:], gx) and not dx[:, :-100].any()
+    assert ((dw - gw).abs() <= 1e-5 * (1 + gw.abs())).all() and ((db - gb).abs() <= 1e-5 * (1 + gb.abs())).all()  # 50 terms in another order
+    del dx, dy, y
+    # decays of exp(-5) and less a row: 100 rows are all that a state knows of
+    A = -50.0 * (1 + torch.rand(C, 2, device="cuda"))
+    dt = torch.full((1, 1, C), 0.1, device="cuda").bfloat16().expand(1, 1050, C).repeat(1, 1000, 1)
+    B = rand(1, 1050, 2, seed=5, dtype=torch.bfloat16).repeat(1, 1000, 1)
+    y, last = la.selective_scan(x, dt, A, B, B, step="value")
+    z, last2 = la.selective_scan(x[:, -200:].contiguous(), dt[:, -200:].contiguous(), A, B[:, -200:].contiguous(), B[:, -200:].contiguous(), step="value")
+    assert torch.equal(y[:, -64:], z[:, -64:]) or ((y[:, -64:] - z[:, -64:]).float().abs() <= 2.0 ** -8 * (1 + z[:, -64:].float().abs())).all()
+    assert ((last - last2).abs() <= 1e-5 * (1 + last2.abs())).all()
+    leaf = [t.detach().requires_grad_(True) for t in (x, dt, A, B, B)]
+    dy = torch.zeros_like(x)
+    dy[:, -50:] = rand(1, 50, C, seed=6, dtype=torch.bfloat16)
+    o, _ = la.selective_scan(*leaf, step="value")
+    got = torch.autograd.grad(o, leaf, dy)
+    short = [t.detach()[:, -200:].contiguous().requires_grad_(True) if t.dim() == 3 else t.detach().requires_grad_(True) for t in leaf]
+    o, _ = la.selective_scan(*short, step="value")
+    want = torch.autograd.grad(o, short, dy[:, -200:])
+    for a, c in zip(got, want):
+        a = a[:, -200:] if a.dim() == 3 else a
+        near = (a.float() - c.float()).abs() <= 2.0 ** -7 * c.float().abs() + 1e-4 * c.float().abs().max()
+        assert near[:, -64:].all() if a.dim() == 3 else near.all()
