@@ -195,13 +195,20 @@ __device__ __forceinline__ float sum_all(float v, const float (&x)[P])
 }
 #undef LA_OF_LANE
 
+// A[s] in powers of two.  Finite, where it is not NaN, so that a row that is not there (d = 0) leaves the state as it is; below
+// the lowest number any d > 2^-120 forgets the state.
+__device__ __forceinline__ float decay_of(float A)
+{
+    const float x = A * kLog2e, low = -0x1.fffffep127f;
+    return x < low ? low : x;
+}
 template <int P>
 __device__ __forceinline__ void decays(const Scan &a, const Spot &p, int wave, float (&A)[P])
 {
 #pragma unroll
     for (int j = 0; j < P; ++j) {
         const int s = wave * P + j;
-        A[j] = s < a.S ? a.A[(size_t)p.c * a.S + s] * kLog2e : 0.f;
+        A[j] = s < a.S ? decay_of(a.A[(size_t)p.c * a.S + s]) : 0.f;
     }
 }
 // The states that the walk starts from: the caller's, or those that k_selective_chain left for the segment.
@@ -245,7 +252,7 @@ __global__ void __launch_bounds__(256) k_selective_chain(Scan a)
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
     if (i >= (size_t)a.B * a.S * a.C) return;
     const int c = (int)(i % a.C), s = (int)(i / a.C % a.S), b = (int)(i / a.C / a.S);
-    const float A = a.A[(size_t)c * a.S + s] * kLog2e;
+    const float A = decay_of(a.A[(size_t)c * a.S + s]);
     float h = a.first ? a.first[((size_t)b * a.C + c) * a.S + s] : 0.f;
     constexpr int AHEAD = 16;  // segments whose words are asked for together
     for (int k0 = 0; k0 < a.segs; k0 += AHEAD) {
@@ -428,7 +435,7 @@ __device__ __forceinline__ float4 over_lanes(float (&v)[64])
 // Backward.  FULL: outputs, walking the tiles from the far end: states from the saved ones before the tile on, then the rows in
 // reverse.  Else what the segment hands to the rows before it from nothing behind it.
 template <typename T, int P, int W, bool FULL>
-__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(FULL ? (W == 12 || W == 6 ? 3 : W == 16 || W == 8 ? 4 : 3) : 4))) k_selective_back(Scan a)
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(FULL && W % 8 ? 3 : 4))) k_selective_back(Scan a)
 {
     constexpr int OWN = (kPairs + W - 1) / W, PART = kCells / P, PARTS = kRows / PART;
     __shared__ float4 du[kPairs][64];
@@ -715,7 +722,7 @@ __global__ void __launch_bounds__(256) k_selective_step(Scan a, float *state, in
 #pragma unroll
     for (int j = 0; j < P; ++j) {
         const int s = l * P + j;
-        A[j] = s < a.S ? a.A[(size_t)c * a.S + s] * kLog2e : 0.f;
+        A[j] = s < a.S ? decay_of(a.A[(size_t)c * a.S + s]) : 0.f;
         h[j] = s < a.S ? state[k * a.S + s] : 0.f;
     }
     const float bias = a.bias ? a.bias[c] : 0.f, D = a.D ? a.D[c] : 0.f;
@@ -751,8 +758,8 @@ Shape shape_of(int S, bool two)
     if (S <= 64) return {4, S <= 16 ? 4 : S <= 24 ? 6 : S <= 32 ? 8 : S <= 48 ? 12 : 16};
     return {8, S <= 96 ? 12 : 16};
 }
-// f(states as a constant, waves as a constant)
-template <typename F>
+// f(states as a constant, waves as a constant).  TWO: also the shapes of two states a wave for more than 8.
+template <bool TWO, typename F>
 void by_shape(const Shape &s, F f)
 {
     auto with = [&](auto P, auto W) {
@@ -764,8 +771,10 @@ void by_shape(const Shape &s, F f)
     with(two, std::integral_constant<int, 1>());
     with(two, two);
     with(two, four);
-    with(two, std::integral_constant<int, 6>());
-    with(two, eight);
+    if constexpr (TWO) {
+        with(two, std::integral_constant<int, 6>());
+        with(two, eight);
+    }
     with(four, four);
     with(four, std::integral_constant<int, 6>());
     with(four, eight);
@@ -929,21 +938,20 @@ la_status la_selective_forward(const void *X, size_t x_stride, const void *Dt, s
     a.sums = (float *)workspace + room.sums, a.spans = (float *)workspace + room.spans;
     const dim3 grid((unsigned)((size_t)B * a.columns * a.segs)), chain((unsigned)(((size_t)B * C * S + 255) / 256));
     const hipStream_t st = (hipStream_t)hip_stream;
-    la::by_shape(shape, [&](auto P, auto W) {
+    auto run = [&](auto *t, auto P, auto W) {
+        using T = std::remove_pointer_t<decltype(t)>;
         constexpr int p = decltype(P)::value, w = decltype(W)::value;
-        if (dt == LA_F32) {
+        if constexpr (p > 2 || w <= 4) {  // (else two states a wave of one piece: lay_out)
             if (a.segs > 1) {
-                la::k_selective<float, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective<T, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
                 la::k_selective_chain<false><<<chain, dim3(256), 0, st>>>(a);
             }
-            la::k_selective<float, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
-        } else {
-            if (a.segs > 1) {
-                la::k_selective<la::bf16_t, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
-                la::k_selective_chain<false><<<chain, dim3(256), 0, st>>>(a);
-            }
-            la::k_selective<la::bf16_t, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
         }
+        la::k_selective<T, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
+    };
+    la::by_shape<true>(shape, [&](auto P, auto W) {
+        if (dt == LA_F32) run((float *)nullptr, P, W);
+        else run((la::bf16_t *)nullptr, P, W);
     });
     return la::done();
 }
@@ -981,21 +989,18 @@ la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, 
     a.dA = dA ? ws + room.dA : nullptr, a.dd = ws + room.dd;
     const dim3 grid((unsigned)((size_t)B * a.columns * a.segs)), chain((unsigned)(((size_t)B * C * S + 255) / 256));
     const hipStream_t st = (hipStream_t)hip_stream;
-    la::by_shape(shape, [&](auto P, auto W) {
+    auto run = [&](auto *t, auto P, auto W) {
+        using T = std::remove_pointer_t<decltype(t)>;
         constexpr int p = decltype(P)::value, w = decltype(W)::value;
-        if (dt == LA_F32) {
-            if (a.segs > 1) {
-                la::k_selective_back<float, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
-                la::k_selective_chain<true><<<chain, dim3(256), 0, st>>>(a);
-            }
-            la::k_selective_back<float, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
-        } else {
-            if (a.segs > 1) {
-                la::k_selective_back<la::bf16_t, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
-                la::k_selective_chain<true><<<chain, dim3(256), 0, st>>>(a);
-            }
-            la::k_selective_back<la::bf16_t, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
+        if (a.segs > 1) {
+            la::k_selective_back<T, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+            la::k_selective_chain<true><<<chain, dim3(256), 0, st>>>(a);
         }
+        la::k_selective_back<T, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
+    };
+    la::by_shape<false>(shape, [&](auto P, auto W) {
+        if (dt == LA_F32) run((float *)nullptr, P, W);
+        else run((la::bf16_t *)nullptr, P, W);
     });
     const dim3 all = la::blocks_of((size_t)B * G * a.tiles * la::shares_of(shape));
     if (dt == LA_F32) la::k_selective_shares<float><<<all, dim3(256), 0, st>>>(a, (float *)dBm, (float *)dCm, shape.P, shape.W);

@@ -142,3 +142,24 @@ def test_extremes(step):
     A[:, 3] = 0.0
     A[:, 4] = -1e4
     check(x, dt, A, Bm, Cm, D, bias, h0, dy, dlast, None, step)
+
+
+@pytest.mark.parametrize("N", [40, 700])
+def test_decays_to_nothing_at_once(N):
+    """A of minus infinity forgets the state at every row and, like any other, leaves it alone behind a sequence's end:
+    the same bits as with a decay that is as good as that."""
+    x, dt, A, Bm, Cm, D, bias, h0, dy, dlast = draw(4, N, 70, 16, 1, "f32", "softplus", N)
+    n = torch.tensor([N, 17, 0, N - 30], dtype=torch.int32).cuda()
+    results = []
+    for low in (-float("inf"), -1e30):
+        A[:, 5] = low
+        A[3, :] = low
+        ins = up(x, dt, A, Bm, Cm, D, bias)
+        y, last, saved = forward(*ins, *up(h0), n, "softplus")
+        got = backward(*ins, saved, *up(dy, dlast), n, "softplus")
+        state, z = last.clone(), poison((4, 1, 70), F)
+        la.la_selective_step(*[t[:, :1].contiguous() for t in ins[:2]], ins[2], *[t[:, :1].contiguous() for t in ins[3:5]], *ins[5:], state, z,
+                             la.LA_STEP_SOFTPLUS)
+        results.append([y, last, state, z, *got.values()])
+    for a, b in zip(*results):
+        assert torch.isfinite(a).all() and torch.equal(a, b)
