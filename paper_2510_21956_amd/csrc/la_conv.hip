@@ -4,7 +4,9 @@
 // registers: every row is read once, but for the W - 1 rows in front of a run.  Rows may start at any element: the
 // lane at a row's end takes its last V channels once more.
 //
-// Bound by HBM: 2 W + 8 operations a row and channel for two tensors moved forward and three backward.
+// Bound by HBM: 2 W operations and the activation a row and channel, twice to three times that backward, for two tensors
+// moved forward and three backward.  8 x 2048 rows of 2048 channels, 4 taps, bf16: forward 28 us, 4.8 TB/s; backward 55,
+// 3.7 TB/s, with the join of dw 4 of them; 32 x 2048 of 4096, 213 and 351, 5.0 and 4.6 TB/s.
 #include "la_checks.h"
 #include "la_common.h"
 #include "la_scalar.h"
@@ -161,7 +163,7 @@ __global__ void __launch_bounds__(256) k_conv(Conv a)
 // Backward.  A workgroup's four waves take runs of rows that follow one another, `lanes` lanes to a run; e of the W - 1
 // rows behind a run is formed once more.  Sums of dw and dbias: a lane's rows, then the runs of a wave and of the
 // workgroup, whose share k_conv_join adds to the others'.
-template <typename T, typename WT, int V, int W, int ACT>
+template <typename T, typename WT, int V, int W, int U, int ACT>
 __global__ void __launch_bounds__(256) k_conv_back(Conv a)
 {
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, per = 64 / a.lanes;
@@ -187,7 +189,6 @@ __global__ void __launch_bounds__(256) k_conv_back(Conv a)
             for (int j = 0; j < W - 1; ++j) past[j] = widened(row_at<T, V, W>(a, b, t0 - (W - 1) + j, c));
         const T *X = (const T *)a.X + row0 * a.xs + c, *dY = (const T *)a.dY + row0 * a.C + c;
         T *dX = (T *)a.dX + row0 * a.C + c;
-        constexpr int U = rows_together<W>;
         Piece<T, V> nx[U], ny[U];
 #pragma unroll
         for (int k = 0; k < U; ++k)
@@ -339,17 +340,22 @@ __global__ void __launch_bounds__(256) k_conv_step(Conv a)
 constexpr int kMostTaps = 8;
 
 // Channels a lane takes: four, two where the taps would fill the registers, backward two; one where a row is shorter.  More of
-// them leave fewer waves, whose loads are not enough: 8 x 2048 rows of 2048, bf16, forward 29 us, with eight 36; backward
-// 58, with four 59 and with eight 76.
+// them leave fewer waves, whose loads are not enough: 8 x 2048 rows of 2048, bf16, forward 28 us, with eight 36; backward
+// 55, with four 74 and with eight 85.
 template <int W>
 constexpr int wide_of = W > 4 ? 2 : 4;
 constexpr int kWideBack = 2;
 
-// Rows of a run: enough waves to fill the chip, and few rows read twice.
-int run_rows(int B, int N, size_t pieces)
+// Backward, up to four taps: twice the rows together where a run has as many as this (8 x 2048 rows of 2048, runs of 64:
+// 55 us, else 60; 2 x 3001 rows, runs of 32: 26 us, with twice the rows together 27).
+constexpr int kLongRun = 64;
+
+// Rows of a run: enough waves to fill the chip, and few rows read twice.  4096 waves forward, 2048 backward, whose rows
+// behind a run cost more (2 x 3001 rows of 2048, bf16: 13 us forward, with 2048 waves 14; 26 backward, with 4096 32).
+int run_rows(int B, int N, size_t pieces, int waves)
 {
     int run = 128;
-    while (run > 16 && (double)B * ((N + run - 1) / run) * pieces < 64.0 * 4096) run /= 2;
+    while (run > 16 && (double)B * ((N + run - 1) / run) * pieces < 64.0 * waves) run /= 2;
     return run;
 }
 
@@ -398,7 +404,7 @@ Back back_of(int B, int N, int C, int most)
     p.lanes = 1;
     while (p.lanes < 64 && p.lanes < pieces) p.lanes *= 2;
     p.columns = (pieces + p.lanes - 1) / p.lanes;
-    p.run = run_rows(B, N, (size_t)p.columns * p.lanes);
+    p.run = run_rows(B, N, (size_t)p.columns * p.lanes, 2048);
     p.runs = (N + p.run - 1) / p.run;
     const int of = 4 * (64 / p.lanes);
     p.count = (int)(((size_t)B * p.runs + of - 1) / of);
@@ -440,7 +446,7 @@ la_status la_conv_forward(const void *X, size_t x_stride, const void *Wt, const 
         auto go = [&](auto wide) {
             constexpr int U = decltype(wide)::value;
             const size_t each = (C + U - 1) / U;
-            a.run = la::run_rows(B, N, each);
+            a.run = la::run_rows(B, N, each, 4096);
             a.runs = (N + a.run - 1) / a.run;
             a.items = (size_t)B * a.runs * each;
             const size_t all = a.items + (last ? (size_t)B * (K - 1) * each : 0);
@@ -483,11 +489,15 @@ la_status la_conv_backward(const void *X, size_t x_stride, const void *Wt, const
         constexpr int K = decltype(taps)::value, V = la::kWideBack;
         const la::Back p = la::back_of(B, N, C, V);
         a.lanes = p.lanes, a.columns = p.columns, a.run = p.run, a.runs = p.runs;
-        auto go = [&](auto wide) {
-            la::k_conv_back<T, WT, decltype(wide)::value, K, decltype(act_)::value><<<dim3((unsigned)p.columns * p.count), dim3(256), 0, st>>>(a);
+        auto go = [&](auto wide, auto rows) {
+            la::k_conv_back<T, WT, decltype(wide)::value, K, decltype(rows)::value, decltype(act_)::value>
+                <<<dim3((unsigned)p.columns * p.count), dim3(256), 0, st>>>(a);
         };
-        if (C >= V) go(std::integral_constant<int, V>());
-        else go(std::integral_constant<int, 1>());
+        const std::integral_constant<int, la::rows_together<K>> few;
+        const std::integral_constant<int, la::rows_together<K> * (K > 4 ? 1 : 2)> many;
+        if (C < V) go(std::integral_constant<int, 1>(), few);
+        else if (p.run >= la::kLongRun) go(std::integral_constant<int, V>(), many);
+        else go(std::integral_constant<int, V>(), few);
         if (need) la::k_conv_join<K><<<dim3((C + 63) / 64, K + 1), dim3(1024), 0, st>>>(a.shares, dW, dbias, p.count, C);
     });
     return la::done();

@@ -82,6 +82,13 @@ def test_padded_batches(N, C, lengths, W, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("W", [2, 3, 4, 5])
+def test_many_channels_and_rows(W, dtype):
+    """Enough of both for runs of 64 rows and more, which take more rows together; ends inside a run, and whole runs behind an end."""
+    check(*draw(3, 1400, 4099, W, dtype, "f32", W), torch.tensor([1400, 1000, 37], dtype=torch.int32), "silu")
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("C,wide,at", [(64, 200, 3), (24, 25, 1), (5, 40, 7)])
 def test_parts_of_wider_rows(C, wide, at, dtype):
     """x is read where it stands, at any element; what is beside it is not."""
