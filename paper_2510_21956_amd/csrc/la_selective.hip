@@ -2,9 +2,20 @@
 // in steps.
 //
 // A lane holds one channel, a wave P of its states in registers, a workgroup's W waves all S <= P W of them; it walks a
-// sequence (or a segment of one) in tiles of rows.  The waves share a tile's rows: each forms d and d x of its rows
-// and leaves them in LDS, with the tile's B and C; then every wave walks all rows with its states, and at last each
-// wave adds up the waves' shares of its rows' outputs.
+// sequence (or a segment of one) in tiles of 16 rows.  The waves share a tile's rows: each forms d and d x of its rows
+// and leaves them in LDS; then every wave walks all rows with its states, and at last each wave adds up the waves'
+// shares of its rows' outputs.  B and C of a row are the same for all channels: a wave keeps a tile's as one value a lane, and the
+// instruction that needs one reads the lane that has it (through LDS every wave would read them back 64 times over; through
+// scalar loads 8 x 2048 rows took 373 us, this way 302 when both were tried).  Where there are few sequences and channels,
+// these are cut into segments, walked side by side from zero states first to learn where each of them starts (lay_out).
+//
+// The backward pass goes by the states before every tile, which the forward pass keeps (S / 4 bytes an element of X): a
+// tile is walked forward once more, half of it at a time with all its states and decays in registers, then back.
+//
+// Bound by the vector ALU: a state and row of 64 channels takes 21 cycles of a SIMD forward (an exponential 7, two products, a
+// sum, the read-out; reading another lane's value doubles an instruction's time) and 65 backward (states one and a half times, eight operations,
+// sums over the channels 16 to 19).  8 x 2048 rows of 2048 channels, 16 states, bf16: 82 and 254 us of that at 2.1 GHz, 105 us of bytes,
+// 222 and 530 measured (there are 256 chains, two waves to a SIMD forward); 64 x 512 rows, 164 and 508, 257 and 775.
 #include "la_checks.h"
 #include "la_common.h"
 #include "la_scalar.h"
@@ -434,8 +445,11 @@ __device__ __forceinline__ float4 over_lanes(float (&v)[64])
 
 // Backward.  FULL: outputs, walking the tiles from the far end: states from the saved ones before the tile on, then the rows in
 // reverse.  Else what the segment hands to the rows before it from nothing behind it.
+// Registers, of as many waves to a SIMD as the attribute says: 168 for three (four or six waves a workgroup spill 16 to 20 bytes a
+// lane, for 170 and two waves they would not); eight waves, of which four to a SIMD would have 128 and spill 136 bytes, run
+// two to a SIMD (4 x 2048 rows of 1024, 32 states, fp32: 280 us, with four 379); 16 waves a workgroup can't have more than 128.
 template <typename T, int P, int W, bool FULL>
-__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(FULL && W % 8 ? 3 : 4))) k_selective_back(Scan a)
+__global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FULL || W == 16 ? 4 : W == 8 ? 2 : 3))) k_selective_back(Scan a)
 {
     constexpr int OWN = (kPairs + W - 1) / W, PART = kCells / P, PARTS = kRows / PART;
     __shared__ float4 du[kPairs][64];
@@ -752,14 +766,17 @@ __global__ void __launch_bounds__(256) k_selective_step(Scan a, float *state, in
 struct Shape {
     int P, W;
 };
-Shape shape_of(int S, bool two)
+// Backward, 16 waves have too few registers for four states each (128, 136 bytes of spills a lane): more than 48 states take
+// 8 waves of eight.  2 x 2048 rows of 1024, 64 states, fp32: 320 us, with 16 waves 369; 16 x 1024, bf16: 955 and 1113.
+Shape shape_of(int S, bool two, bool backward)
 {
+    if (backward && S > 48 && S <= 64) return {8, 8};
     if (S <= 8 || (S <= 16 && two)) return {2, S <= 2 ? 1 : S <= 4 ? 2 : S <= 8 ? 4 : S <= 12 ? 6 : 8};
     if (S <= 64) return {4, S <= 16 ? 4 : S <= 24 ? 6 : S <= 32 ? 8 : S <= 48 ? 12 : 16};
     return {8, S <= 96 ? 12 : 16};
 }
-// f(states as a constant, waves as a constant).  TWO: also the shapes of two states a wave for more than 8.
-template <bool TWO, typename F>
+// f(states as a constant, waves as a constant), of the shapes that the pass takes
+template <bool BWD, typename F>
 void by_shape(const Shape &s, F f)
 {
     auto with = [&](auto P, auto W) {
@@ -771,15 +788,16 @@ void by_shape(const Shape &s, F f)
     with(two, std::integral_constant<int, 1>());
     with(two, two);
     with(two, four);
-    if constexpr (TWO) {
+    if constexpr (BWD) with(eight, eight);
+    else {
         with(two, std::integral_constant<int, 6>());
         with(two, eight);
+        with(four, std::integral_constant<int, 16>());
     }
     with(four, four);
     with(four, std::integral_constant<int, 6>());
     with(four, eight);
     with(four, std::integral_constant<int, 12>());
-    with(four, std::integral_constant<int, 16>());
     with(eight, std::integral_constant<int, 12>());
     with(eight, std::integral_constant<int, 16>());
 }
@@ -826,7 +844,7 @@ struct Inputs {
 // find (what every segment makes of zero states, an exponential and three operations for every row and state once more, and
 // the walk along the segments).  512 rows take, in us, with w waves on every SIMD of the busiest compute units (S = 16, bf16):
 // 39 + 29 w forward (31 + 35 w with two states a wave), 100 + 80 w backward, what the segments make of zero states 28 + 23 w and 31 + 21 w.  Segments fill the
-// compute units once forward, about twice backward (5 and 3 or 4 waves to a SIMD at once), and have 32 rows at least; one
+// compute units once forward, about twice backward (5 waves to a SIMD at once, backward 2 to 4), and have 32 rows at least; one
 // piece where that takes less.  Of 1 to 96 segments, on 10 shapes of 1 to 256 chains, this takes 1.04 times the best on the average.
 // Forward, one piece and few waves: two states a wave instead of four, whose twice as many waves hide each other's
 // waits (8 x 2048 rows of 2048 channels 228 us, with four 260, in 8 segments 240).
@@ -836,10 +854,10 @@ Shape lay_out(Scan &a, bool backward)
     a.per = (a.group + 63) / 64;
     a.columns = a.G * a.per;
     a.tiles = (a.N + kRows - 1) / kRows;
-    const Shape s = shape_of(a.S, false);
+    const Shape s = shape_of(a.S, false, backward);
     const double chains = (double)a.B * a.columns, waves = chains * s.W / 1024.0, rows = a.N / 512.0;
-    const int slots = 256 * ((backward ? s.W % 8 ? 12 : 16 : 20) / s.W);  // workgroups at once
-    const int rounds = (int)((backward ? 1792.0 : 1536.0) * 4 / s.W / slots + 0.4);
+    const int slots = 256 * ((!backward ? 20 : s.W == 16 ? 16 : s.W == 8 ? 8 : 12) / s.W);  // workgroups at once
+    const int rounds = (int)((!backward ? 1536.0 : s.W == 8 ? 1024.0 : 1792.0) * 4 / s.W / slots + 0.4);
     const double most = (rounds ? rounds : 1) * (double)slots / chains;
     int segs = (int)(most < 256.0 ? most : 256.0);
     if (segs > a.N / 32) segs = a.N / 32;
@@ -851,7 +869,7 @@ Shape lay_out(Scan &a, bool backward)
     const int of = (a.tiles + segs - 1) / segs;
     a.seg = of * kRows;
     a.segs = (a.tiles + of - 1) / of;
-    return shape_of(a.S, two && a.segs == 1);
+    return shape_of(a.S, two && a.segs == 1, backward);
 }
 Scan scan_of(const void *X, size_t xs, const void *Dt, size_t ts, const float *A, const void *Bm, size_t bs, const void *Cm, size_t cs,
              const float *D, const float *bias, int B, int N, int C, int S, int G, la_step step)
@@ -949,7 +967,7 @@ la_status la_selective_forward(const void *X, size_t x_stride, const void *Dt, s
         }
         la::k_selective<T, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
     };
-    la::by_shape<true>(shape, [&](auto P, auto W) {
+    la::by_shape<false>(shape, [&](auto P, auto W) {
         if (dt == LA_F32) run((float *)nullptr, P, W);
         else run((la::bf16_t *)nullptr, P, W);
     });
@@ -998,7 +1016,7 @@ la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, 
         }
         la::k_selective_back<T, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
     };
-    la::by_shape<false>(shape, [&](auto P, auto W) {
+    la::by_shape<true>(shape, [&](auto P, auto W) {
         if (dt == LA_F32) run((float *)nullptr, P, W);
         else run((la::bf16_t *)nullptr, P, W);
     });

@@ -163,3 +163,9 @@ def test_decays_to_nothing_at_once(N):
         results.append([y, last, state, z, *got.values()])
     for a, b in zip(*results):
         assert torch.isfinite(a).all() and torch.equal(a, b)
+
+
+@pytest.mark.parametrize("S", [2, 4, 13, 24, 30, 40, 60, 90, 128])
+def test_segments_of_every_number_of_states(S):
+    """Few channels and many rows, which are walked in segments, one sequence ending inside one."""
+    check(*draw(2, 333, 20, S, 1, "f32", "softplus", S), torch.tensor([333, 170], dtype=torch.int32), "softplus")
