@@ -11,7 +11,7 @@ raw rows.  a and b are constants.
 
 The operators around the attention follow below it in the same manner: gated_recurrence, rms_norm, and
 rows in 8 bits (pack_rows, unpack_rows, rms_norm_quantised, the ``checkpoint`` of linear_attention and
-rms_norm).
+rms_norm); behind them a selective state space layer's: causal_conv, selective_scan.
 
 Every call can be captured into a graph, a training step too: run it a few times on the stream that will capture,
 let go of the results (no eager graph of the same leaves may be alive while a backward pass is captured: torch

@@ -346,7 +346,7 @@ template <int W>
 constexpr int wide_of = W > 4 ? 2 : 4;
 constexpr int kWideBack = 2;
 
-// Backward, up to four taps: twice the rows together where a run has as many as this (8 x 2048 rows of 2048, runs of 64:
+// Backward, up to four taps: twice the rows together where a run has as many as this (8 x 2048 rows of 2048, runs of 128:
 // 55 us, else 60; 2 x 3001 rows, runs of 32: 26 us, with twice the rows together 27).
 constexpr int kLongRun = 64;
 

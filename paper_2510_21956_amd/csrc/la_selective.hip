@@ -15,7 +15,7 @@
 // Bound by the vector ALU: a state and row of 64 channels takes 21 cycles of a SIMD forward (an exponential 7, two products, a
 // sum, the read-out; reading another lane's value doubles an instruction's time) and 65 backward (states one and a half times, eight operations,
 // sums over the channels 16 to 19).  8 x 2048 rows of 2048 channels, 16 states, bf16: 82 and 254 us of that at 2.1 GHz, 105 us of bytes,
-// 222 and 530 measured (there are 256 chains, two waves to a SIMD forward); 64 x 512 rows, 164 and 508, 257 and 775.
+// 222 and 485 measured (there are 256 chains, two waves to a SIMD); 64 x 512 rows, 164 and 508, 257 and 775.
 #include "la_checks.h"
 #include "la_common.h"
 #include "la_scalar.h"
@@ -791,9 +791,9 @@ void by_shape(const Shape &s, F f)
     if constexpr (BWD) with(eight, eight);
     else {
         with(two, std::integral_constant<int, 6>());
-        with(two, eight);
         with(four, std::integral_constant<int, 16>());
     }
+    with(two, eight);
     with(four, four);
     with(four, std::integral_constant<int, 6>());
     with(four, eight);
@@ -843,11 +843,12 @@ struct Inputs {
 // How a call is laid out: the states of a wave, and the segments that sequences are cut into, whose start states two more launches
 // find (what every segment makes of zero states, an exponential and three operations for every row and state once more, and
 // the walk along the segments).  512 rows take, in us, with w waves on every SIMD of the busiest compute units (S = 16, bf16):
-// 39 + 29 w forward (31 + 35 w with two states a wave), 100 + 80 w backward, what the segments make of zero states 28 + 23 w and 31 + 21 w.  Segments fill the
+// 39 + 29 w forward (31 + 35 w with two states a wave), 100 + 80 w backward (5 + 117 w), what the segments make of zero states 28 + 23 w and 31 + 21 w.  Segments fill the
 // compute units once forward, about twice backward (5 waves to a SIMD at once, backward 2 to 4), and have 32 rows at least; one
 // piece where that takes less.  Of 1 to 96 segments, on 10 shapes of 1 to 256 chains, this takes 1.04 times the best on the average.
-// Forward, one piece and few waves: two states a wave instead of four, whose twice as many waves hide each other's
-// waits (8 x 2048 rows of 2048 channels 228 us, with four 260, in 8 segments 240).
+// One piece and few waves: two states a wave instead of four, whose twice as many waves hide each other's
+// waits (8 x 2048 rows of 2048 channels 222 us forward, with four 260, in 8 segments 240; backward 484, in 3 segments
+// 546; with 12 states backward 543 and 529: only from 13 on).
 Shape lay_out(Scan &a, bool backward)
 {
     a.group = a.C / a.G;
@@ -862,8 +863,9 @@ Shape lay_out(Scan &a, bool backward)
     int segs = (int)(most < 256.0 ? most : 256.0);
     if (segs > a.N / 32) segs = a.N / 32;
     const double busiest = (double)(int)((chains + 255) / 256) * s.W / 4.0;
-    const bool two = !backward && a.S <= 16 && 31 + 35 * busiest < 39 + 29 * busiest;
-    const double whole = rows * (backward ? 100 + 80 * busiest : two ? 31 + 35 * busiest : 39 + 29 * busiest);
+    const double fours = backward ? 100 + 80 * busiest : 39 + 29 * busiest, twos = backward ? 5 + 117 * busiest : 31 + 35 * busiest;
+    const bool two = a.S <= 16 && (a.S > 12 || !backward) && twos < fours;
+    const double whole = rows * (two ? twos : fours);
     const double cut = 8.0 + rows * (backward ? 101 * waves + 131.0 / segs : 52 * waves + 67.0 / segs);
     if (segs < 2 || whole <= cut) segs = 1;
     const int of = (a.tiles + segs - 1) / segs;
@@ -1010,9 +1012,11 @@ la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, 
     auto run = [&](auto *t, auto P, auto W) {
         using T = std::remove_pointer_t<decltype(t)>;
         constexpr int p = decltype(P)::value, w = decltype(W)::value;
-        if (a.segs > 1) {
-            la::k_selective_back<T, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
-            la::k_selective_chain<true><<<chain, dim3(256), 0, st>>>(a);
+        if constexpr (p > 2 || w <= 4) {
+            if (a.segs > 1) {
+                la::k_selective_back<T, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective_chain<true><<<chain, dim3(256), 0, st>>>(a);
+            }
         }
         la::k_selective_back<T, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
     };
