@@ -803,9 +803,11 @@ def la_rmsnorm_backward(total, scales, weight, rstd, dy, dtotal, dx, dweight, wo
 # ---- the selective state space layer ----------------------------------------------------------
 
 def row_stride(t, dims=1):
-    """Elements from one row of t to the next, a row being its last ``dims`` dimensions; None where rows are not dense, or do not
-    follow one another at one distance, at least their own length."""
+    """Elements from one row of t to the next, a row being its last ``dims`` dimensions; None where t has fewer, where rows are not
+    dense, or do not follow one another at one distance, at least their own length."""
     row, step, sizes, strides = 1, None, t.shape, t.stride()
+    if len(sizes) < dims:
+        return None
     for d in reversed(range(len(sizes) - dims, len(sizes))):
         if sizes[d] != 1 and strides[d] != row:
             return None
