@@ -245,6 +245,19 @@ __device__ __forceinline__ void states_to(float *to, const Scan &a, const Spot &
         if (s < a.S) to[((size_t)p.b * a.C + p.c) * a.S + s] = h[j];
     }
 }
+// The sum of a segment's d from those of its tiles (pairs of rows, then eight of these: 8 U), with what every addition loses: within
+// 10 U of it however many rows the segment has.  One serial sum of a thousand equal d is off by some 250 U, which exp(A sum d) has of
+// a state that the segment carries on.
+struct Span {
+    float large = 0.f, lost = 0.f;
+    __device__ __forceinline__ void add(float x)
+    {
+        const float s = large + x, taken = s - large;
+        lost += (large - (s - taken)) + (x - taken);
+        large = s;
+    }
+    __device__ __forceinline__ float sum() const { return lost == lost ? large + lost : large; }  // infinities lose NaN
+};
 template <int P>
 __device__ __forceinline__ void leave_sums(const Scan &a, const Spot &p, int wave, const float (&h)[P], float span)
 {
@@ -293,7 +306,8 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
     __shared__ float2 ys[FULL ? W : 1][kPairs][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Spot p(a, lane);
-    float A[P], h[P], span = 0.f;
+    float A[P], h[P];
+    Span span;
     decays<P>(a, p, wave, A);
     if (FULL) states_from<P>(a, p, wave, h);
     else
@@ -352,6 +366,7 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
             saved += (size_t)a.S * a.C;
         }
         float4 s = du[0][lane], next = du[1][lane];
+        float of_tile = 0.f;  // the sum of d
         float f[2 * P], g[2 * P];  // exp(d A) of a pair of rows, and of the next
         auto open = [&](float (&f)[2 * P], const float4 &s) {
 #pragma unroll
@@ -369,14 +384,15 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
                     h[j] = fmaf(f[r * P + j], h[j], (r ? s.w : s.y) * of_lane<k % 16 + decltype(j)::value>(B.v[k / 16]));
                 });
                 if (FULL) y[r] = sum_all<k % 16>(C.v[k / 16], h);
-                else span += r ? s.z : s.x;
             });
+            if (!FULL) of_tile += s.x + s.z;
             if (FULL) ys[wave][q][lane] = make_float2(y[0], y[1]);
             s = next, next = after;
 #pragma unroll
             for (int j = 0; j < 2 * P; ++j) f[j] = g[j];
             keep_order();
         });
+        if (!FULL) span.add(of_tile);
         block_sync();
         if (FULL) {
 #pragma unroll
@@ -402,7 +418,7 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
             for (int t = max(p.r0, p.n) + wave; t < min(a.N, p.r0 + a.seg); t += W)  // padding
                 store_elem((T *)a.Y, ((size_t)p.b * a.N + t) * a.C + p.c, 0.f);
         if (p.seg == max(p.n - 1, 0) / a.seg) states_to<P>(a.end, a, p, wave, h);
-    } else leave_sums<P>(a, p, wave, h, span);
+    } else leave_sums<P>(a, p, wave, h, span.sum());
 }
 
 // 64 values a lane, added up over the wave's lanes.  At every step a lane keeps half of its values, by a bit of its
@@ -457,7 +473,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
     __shared__ float4 gs[FULL ? W : 1][kPairs][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Spot p(a, lane);
-    float A[P], carry[P], dA[P], before[P], dD = 0.f, db = 0.f, span = 0.f;
+    float A[P], carry[P], dA[P], before[P], dD = 0.f, db = 0.f;
+    Span span;
     decays<P>(a, p, wave, A);
     if (FULL) states_from<P>(a, p, wave, carry);
 #pragma unroll
@@ -587,6 +604,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
             });
             shares -= W * PARTS * 64;
         } else {
+            float of_tile = 0.f;
             each<kPairs>([&](auto q_) {
                 constexpr int q = kPairs - 1 - decltype(q_)::value;
                 const float4 s = du[q][lane];
@@ -596,9 +614,10 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
                     fma_each<k % 16>(carry, C.v[k / 16], r ? y.y : y.x);
 #pragma unroll
                     for (int j = 0; j < P; ++j) carry[j] *= __builtin_amdgcn_exp2f((r ? s.z : s.x) * A[j]);
-                    span += r ? s.z : s.x;
                 });
+                of_tile += s.x + s.z;
             });
+            span.add(of_tile);
         }
         block_sync();
         if constexpr (FULL) {
@@ -655,7 +674,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
             a.dd[at * 2 * a.C + p.c] = s.x;
             a.dd[(at * 2 + 1) * a.C + p.c] = s.y;
         }
-    } else leave_sums<P>(a, p, wave, carry, span);
+    } else leave_sums<P>(a, p, wave, carry, span.sum());
 }
 
 // dB and dC from the columns' shares: a lane to a value, the columns of a group in order.

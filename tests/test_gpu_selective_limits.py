@@ -1,0 +1,55 @@
+"""The short convolution and the selective scan where their tests against the definition do not go: long segments, layouts of many
+chains, infinities, rows that lie far apart."""
+import pytest
+import torch
+
+import paper_2510_21956_amd as la
+from layer_reference import U
+
+pytestmark = pytest.mark.gpu
+F = torch.float32
+
+
+def poison(*shape, dtype=F):
+    return torch.full(shape, float("nan"), dtype=dtype, device="cuda")
+
+
+def room(n):
+    return torch.full((n,), 0xFF, dtype=torch.uint8, device="cuda") if n else None
+
+
+def rand(*shape, seed=0, dtype=F):
+    return torch.randn(shape, generator=torch.Generator().manual_seed(seed)).to(dtype).cuda()
+
+
+def test_states_carried_through_long_segments():
+    """One state, inputs of zero, equal steps: h_t = h0 exp(A d (t + 1)) and dx_t = d B dlast exp(A d (N - 1 - t)), looked at where a
+    segment starts, forward, and ends, backward.  There a value has gone through k segments, each exp(A sum d), z = A sum d = -1/4:
+    the sum's 10 U, A's roundings and the product's 3 U of |z|, the exponential and the product with the state 3 U; then a row's
+    exponential and the read-out's products, 8 U."""
+    N, C, S, segs = 256 * 1232, 64, 1, 256
+    words = la.la_selective_workspace_bytes(1, N, C, S, 1, 0) // 4
+    assert words == segs * C * (S + 1)  # what a segment makes of zero states, and its sum of d
+    assert la.la_selective_workspace_bytes(1, N, C, S, 1, 1) // 4 == segs * C * (2 * S + 3) + N // 16 * 64
+    rows = N // segs
+    d = torch.tensor(0.01)
+    x, dt = torch.zeros(1, N, C, device="cuda"), d.cuda().expand(1, N, C).contiguous()
+    A = torch.full((C, S), -0.25 / (0.01 * rows), device="cuda")
+    Bm, Cm = rand(1, N, S, seed=1), rand(1, N, S, seed=2)
+    h0, dlast = rand(1, C, S, seed=3), rand(1, C, S, seed=4)
+    y, last = poison(1, N, C), poison(1, C, S)
+    saved = room(la.la_selective_saved_bytes(1, N, C, S))
+    la.la_selective_forward(x, dt, A, Bm, Cm, None, None, h0, y, last, saved, None, la.LA_STEP_VALUE,
+                            room(la.la_selective_workspace_bytes(1, N, C, S, 1, 0)))
+    z = A.double()[:, 0] * d.double().item()  # of a row
+    k = torch.arange(segs, dtype=torch.float64, device="cuda").unsqueeze(1)
+    allowed = (k * (13 / 4 + 3) + 8) * U
+    starts = torch.arange(segs, device="cuda") * rows
+    want = Cm[0, starts].double() * h0[0, :, 0].double() * torch.exp(z * (starts + 1.0).unsqueeze(1))
+    assert ((y[0, starts].double() - want).abs() <= allowed * want.abs()).all()
+    dx, ddt, dB, dC = poison(1, N, C), poison(1, N, C), poison(1, N, S), poison(1, N, S)
+    la.la_selective_backward(x, dt, A, Bm, Cm, None, None, saved, x, dlast, dx, ddt, None, dB, dC, None, None, None, None, la.LA_STEP_VALUE,
+                             room(la.la_selective_workspace_bytes(1, N, C, S, 1, 1)))
+    ends = N - 1 - starts
+    want = d.double().item() * Bm[0, ends].double() * dlast[0, :, 0].double() * torch.exp(z * (N - 1.0 - ends).unsqueeze(1))
+    assert ((dx[0, ends].double() - want).abs() <= allowed * want.abs()).all()
