@@ -306,9 +306,9 @@ def rms_norm_quantised(x, weight=None, residual=None, eps=1e-6, code="e4m3"):
 
 # ---- the selective state space layer ----------------------------------------------------------
 
-def _rows_in_place(t, dims=1):
-    """t as the kernels take it: rows that are dense and at one distance, else a copy."""
-    return t if t is None or _b.row_stride(t, dims) is not None else t.contiguous()
+def _rows_in_place(t, dims=1, below=1 << 62):
+    """t as the kernels take it: rows that are dense and at one distance, less than `below` elements, else a copy."""
+    return t if t is None or (_b.row_stride(t, dims) or below) < below else t.contiguous()
 
 
 def _dense(t):
@@ -378,7 +378,7 @@ class SelectiveScanFunction(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, dt, A, B, C, D, bias, h0, lengths, step, keeps):
         dims = 1 if B.dim() == x.dim() else 2
-        x, dt, B, C = _rows_in_place(x), _rows_in_place(dt), _rows_in_place(B, dims), _rows_in_place(C, dims)
+        x, dt, B, C = (_rows_in_place(t, k, _b.ROWS_APART) for t, k in ((x, 1), (dt, 1), (B, dims), (C, dims)))
         A, D, bias, h0, lengths = map(_dense, (A, D, bias, h0, lengths))
         sizes = _scan_sizes(x, A, B)
         y = torch.empty(x.shape, dtype=x.dtype, device=x.device)
@@ -423,7 +423,7 @@ def scan_backward(x, dt, A, B, C, D, bias, lengths, saved, dy, dlast, step, want
 def selective_scan(x, dt, A, B, C, D=None, bias=None, h0=None, lengths=None, step="softplus"):
     """Differentiable selective state space scan along the second to last dimension of x, dt [..., N, C] (float32 or bfloat16
     device tensors), with A [C, S] float32 and B, C [..., N, S], or [..., N, G, S] for G groups of channels, like x; all but A may be
-    parts of wider rows, which are read where they are:
+    parts of wider rows, which are read where they are (copied where they lie 2^24 elements apart or more):
 
       h_t = exp(d_t A) h_{t-1} + d_t x_t B_t,  y_t = sum over the states C_t h_t + D x_t,  with
       step "softplus":  d_t = log(1 + exp(dt_t + bias));   step "value":  d_t = dt_t + bias.

@@ -825,6 +825,21 @@ def row_stride(t, dims=1):
     return step if step >= row else None
 
 
+ROWS_APART = 1 << 24  # what the scan's row strides stay below (la.h)
+
+
+def _near(t, dims, stream):
+    """t, or a copy of it, made on the call's stream, where its rows lie too far apart for the scan: one token out of every sequence of
+    a long batch."""
+    step = None if t is None else row_stride(t, dims)
+    if step is None or step < ROWS_APART or t.is_contiguous():
+        return t
+    if stream is None:
+        return t.detach().contiguous()
+    with torch.cuda.stream(stream):
+        return t.detach().contiguous()
+
+
 def _strided(ref, dims=1, **ts):
     """The row strides of device tensors on ref's device."""
     out = []
@@ -959,7 +974,7 @@ def _selective(x, dt, A, Bm, Cm, D, bias, lengths, states, like):
 
 def la_selective_forward(x, dt, A, Bm, Cm, D, bias, h0, y, last, saved, lengths, step, workspace, stream=None):
     """la_selective_forward of include/la.h: x, dt, y [..., N, C], Bm, Cm [..., N, S] or [..., N, G, S] float32 or bfloat16, all but y
-    parts of wider rows where wanted; A [C, S], D, bias [C] (or None), h0, last [..., C, S] (or None) float32; saved: uint8 device
+    parts of wider rows where wanted (less than 2^24 elements apart); A [C, S], D, bias [C] (or None), h0, last [..., C, S] (or None) float32; saved: uint8 device
     tensor of la_selective_saved_bytes(...) bytes where a backward call follows, or None; lengths [...] int32 or None; step
     LA_STEP_VALUE or LA_STEP_SOFTPLUS; workspace: uint8 device tensor of la_selective_workspace_bytes(..., 0) bytes (None where that
     is 0)."""
@@ -991,10 +1006,12 @@ def la_selective_backward(x, dt, A, Bm, Cm, D, bias, saved, dy, dlast, dx, ddt, 
 
 def la_selective_step(x, dt, A, Bm, Cm, D, bias, state, y, step, stream=None):
     """la_selective_step of include/la.h: x, dt, y [..., T, C], Bm, Cm [..., T, S] or [..., T, G, S]; state [..., C, S] float32, updated
-    in place (as a change that autograd sees, and outside of any graph)."""
+    in place (as a change that autograd sees, and outside of any graph).  Inputs with rows 2^24 elements apart or more are copied first."""
     if _natively("scan_step", "la_selective_step", x, dt, A, Bm, Cm, D, bias, state, y, step, stream):
         return
-    _needed(state=state, y=y)
+    _needed(x=x, dt=dt, B=Bm, C=Cm, state=state, y=y)
+    dims = 1 if Bm.dim() == x.dim() else 2
+    x, dt, Bm, Cm = _near(x, 1, stream), _near(dt, 1, stream), _near(Bm, dims, stream), _near(Cm, dims, stream)
     head, sizes = _selective(x, dt, A, Bm, Cm, D, bias, None, {"state": state}, {"y": y})
     _call("la_selective_step", x, stream, (y, state), *head, _ptr(state), _ptr(y), *sizes, int(step), _real_code(x))
 

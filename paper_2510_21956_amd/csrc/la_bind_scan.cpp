@@ -38,7 +38,12 @@ size_t row_stride(const at::Tensor &t, int dims)
     if (!step) step = std::max(row, (int64_t)1);
     return step >= row ? (size_t)step : 0;
 }
-at::Tensor in_place(const at::Tensor &t, int dims) { return row_stride(t, dims) ? t : t.contiguous(); }
+constexpr size_t kRowsApart = 1 << 24;  // what the scan's row strides stay below (binding.ROWS_APART)
+at::Tensor in_place(const at::Tensor &t, int dims, size_t below = SIZE_MAX)
+{
+    const size_t step = row_stride(t, dims);
+    return step && step < below ? t : t.contiguous();
+}
 
 // A tensor whose rows the kernels read where they are: device, type and sizes as given.
 bool rows_fit(const at::Tensor &t, const at::Tensor &ref, int dims, at::IntArrayRef sizes)
@@ -257,7 +262,8 @@ struct Scan : torch::autograd::Function<Scan> {
     {
         const c10::DeviceGuard guard(x0.device());
         const int dims = B0.dim() > x0.dim() ? 2 : 1;
-        const at::Tensor x = in_place(x0, 1), dt = in_place(dt0, 1), A = A0.contiguous(), Bm = in_place(B0, dims), Cm = in_place(C0, dims);
+        const at::Tensor x = in_place(x0, 1, kRowsApart), dt = in_place(dt0, 1, kRowsApart), A = A0.contiguous(),
+                         Bm = in_place(B0, dims, kRowsApart), Cm = in_place(C0, dims, kRowsApart);
         const Maybe D = packed(D0), bias = packed(bias0), h0 = packed(h00), lengths = packed(lengths0);
         const ScanSizes s(x, A, Bm);
         const at::Tensor y = at::empty(x.sizes(), x.options()), last = at::empty(leading(x, 2, {s.C, s.S}), A.options());
@@ -404,6 +410,7 @@ PyObject *scan_step(PyObject *, PyObject *const *a, Py_ssize_t n)
         for (int i = 1; i < 5; ++i)
             if (is_none(a[i])) Py_RETURN_NONE;
         const ScanCall c(a, Py_None);
+        require(std::max({c.xs, c.ts, c.bs, c.cs}) < kRowsApart);  // the Python function copies
         const la_step step = (la_step)PyLong_AsLong(a[9]);
         void *const st = stream_of(a[10], c.x), *p[9];
         for (int i = 0; i < 9; ++i) p[i] = address(a[i]);

@@ -5,6 +5,7 @@ import torch
 
 import paper_2510_21956_amd as la
 from layer_reference import U
+from paper_2510_21956_amd import binding
 
 pytestmark = pytest.mark.gpu
 F = torch.float32
@@ -53,3 +54,39 @@ def test_states_carried_through_long_segments():
     ends = N - 1 - starts
     want = d.double().item() * Bm[0, ends].double() * dlast[0, :, 0].double() * torch.exp(z * (N - 1.0 - ends).unsqueeze(1))
     assert ((dx[0, ends].double() - want).abs() <= allowed * want.abs()).all()
+
+
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("streams", [False, True])
+def test_tokens_out_of_a_long_batch(monkeypatch, native, streams):
+    """One row of each of two sequences whose rows lie 2^24 elements apart, or a little less: what its copy gives, bit for bit."""
+    la.load_library()
+    if not native:
+        monkeypatch.setattr(binding, "_native", None)
+    C, S = 2048, 16
+    A, D, bias = -torch.exp(rand(C, S, seed=1)), rand(C, seed=2), rand(C, seed=3)
+    for rows in (8192, 8191):
+        hidden = torch.empty(2, rows, C, dtype=torch.bfloat16, device="cuda")
+        proj = torch.empty(2, rows * 8, 256, dtype=torch.bfloat16, device="cuda")
+        x, dt, B, Cm = hidden[:, 5:6], hidden[:, 900:901], proj[:, 3:4, 7:7 + S], proj[:, 9:10, 100:100 + 2 * S].unflatten(2, (2, S))
+        for k, t in enumerate((x, dt, B, Cm)):
+            t.copy_(rand(*t.shape, seed=10 + k, dtype=t.dtype))
+        Cm, B2 = Cm[:, :, 0], Cm
+        stream = torch.cuda.Stream() if streams else None
+        if streams:
+            stream.wait_stream(torch.cuda.current_stream())
+        for b, c in ((B, Cm), (B2, B2)):
+            got = []
+            for place in (lambda t: t, lambda t: t.contiguous()):
+                state, y = rand(2, C, S, seed=20), poison(2, 1, C, dtype=x.dtype)
+                if streams:
+                    torch.cuda.current_stream().synchronize()
+                la.la_selective_step(place(x), place(dt), A, place(b), place(c), D, bias, state, y, la.LA_STEP_SOFTPLUS, stream=stream)
+                if streams:
+                    torch.cuda.current_stream().wait_stream(stream)
+                leaves = [t.detach().requires_grad_(True) for t in (x, dt, b, c)]
+                z, last = la.selective_scan(*(place(t) for t in leaves[:2]), A, *(place(t) for t in leaves[2:]), D, bias, rand(2, C, S, seed=20))
+                grads = torch.autograd.grad([z, last], leaves, [rand(2, 1, C, seed=21, dtype=x.dtype), rand(2, C, S, seed=22)])
+                got.append([state, y, z, last, *grads])
+            assert all(torch.equal(p, q) for p, q in zip(*got)) and torch.isfinite(got[0][1]).all()
+            assert torch.equal(got[0][0], got[0][3])

@@ -4,6 +4,7 @@ import torch
 
 import paper_2510_21956_amd as la
 from paper_2510_21956_amd import binding
+from paper_2510_21956_amd.autograd import _rows_in_place
 from test_selective_layer import _stand_in
 
 
@@ -26,3 +27,19 @@ def test_tensors_without_a_dimension_are_refused_in_words():
                  lambda: la.la_selective_step(x, x, A, B, none, None, None, D(2, 16, 4, t=F), x, 1)):
         with pytest.raises(ValueError):
             call()
+
+
+def test_rows_far_apart_are_copied_for_the_scan():
+    """One row of every sequence of a long batch: the scan takes rows less than 2^24 elements apart, the others are copied, and
+    those alone."""
+    far, near = torch.empty_strided((2, 1, 16), (1 << 24, 16, 1), dtype=torch.bfloat16), torch.zeros(2, 9, 16)[:, 3:4]
+    far.copy_(torch.arange(32.0).reshape(2, 1, 16))
+    for t in (far, far.unflatten(2, (4, 4))):
+        dims = t.dim() - 2
+        assert binding.row_stride(t, dims) == binding.ROWS_APART == 1 << 24
+        for copy in (binding._near(t, dims, None), _rows_in_place(t, dims, binding.ROWS_APART)):
+            assert binding.row_stride(copy, dims) == 16 and torch.equal(copy, t)
+        assert _rows_in_place(t, dims) is t  # the convolution reads them where they are
+    assert binding._near(near, 1, None) is near and _rows_in_place(near, 1, binding.ROWS_APART) is near
+    wide = torch.empty(1, 1, 1 << 24, dtype=torch.bfloat16)  # refused, not copied
+    assert binding._near(wide, 1, None) is wide and binding._near(None, 1, None) is None
