@@ -538,7 +538,7 @@ LA_API la_status la_rmsnorm_backward(const void *S, const void *Sscale, const vo
  *       (a length of 0 or less: `last` is `state`; one of N or more is N).
  *   workspace (only where dW or dbias is wanted): at least la_conv_workspace_bytes(B, N, C, W) bytes, 256-byte aligned.
  * Sums are float32, those of dW and dbias in a fixed order.  Addresses are those of elements.
- * Limits: B, N, C >= 1, N <= 2^30, B * N * x_stride < 2^40, B * C * ceil(N / 16) < 2^31.
+ * Limits: B, N, C >= 1, N <= 2^30, B * N * x_stride < 2^40, B * C * ceil(N / 16) < 2^31, C < 2^31 - 256.
  *
  * la_conv_step appends T rows to the carried ones, which it updates in place: the form for single tokens.  Rows are walked one
  * after another, T is meant to be small.  Calls that share a state must not overlap in time.

@@ -7,6 +7,8 @@
 // Bound by HBM: 2 W operations and the activation a row and channel, twice to three times that backward, for two tensors
 // moved forward and three backward.  8 x 2048 rows of 2048 channels, 4 taps, bf16: forward 28 us, 4.8 TB/s; backward 55,
 // 3.7 TB/s, with the join of dw 4 of them; 32 x 2048 of 4096, 213 and 351, 5.0 and 4.6 TB/s.
+#include <limits.h>
+
 #include "la_checks.h"
 #include "la_common.h"
 #include "la_scalar.h"
@@ -63,6 +65,8 @@ struct Conv {
     size_t xs, items;
     int B, N, C, run, runs, lanes, columns;
 };
+// Pieces of V channels in a row.
+__host__ __device__ __forceinline__ int pieces_of(int C, int V) { return (C - 1) / V + 1; }
 __device__ __forceinline__ int rows_of(const Conv &a, int b)
 {
     return a.lengths ? min(max(a.lengths[b], 0), a.N) : a.N;
@@ -112,7 +116,7 @@ template <typename T, typename WT, int V, int W, int ACT>
 __global__ void __launch_bounds__(256) k_conv(Conv a)
 {
     const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
-    const int pieces = (a.C + V - 1) / V;
+    const int pieces = pieces_of(a.C, V);
     if (i >= a.items) {
         const size_t k = i - a.items;
         if (!a.last || k >= (size_t)a.B * (W - 1) * pieces) return;
@@ -169,8 +173,9 @@ __global__ void __launch_bounds__(256) k_conv_back(Conv a)
     const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, per = 64 / a.lanes;
     const int column = (int)(blockIdx.x % a.columns), share = (int)(blockIdx.x / a.columns);
     const int cv = column * a.lanes + lane % a.lanes;
-    const bool mine = cv * V < a.C;  // else a channel behind the last: that of the lane before
-    const int c = min(cv * V, a.C - V), first = cv * V - c;  // channels before `first` are another lane's
+    const int pieces = pieces_of(a.C, V);
+    const bool mine = cv < pieces;  // else a channel behind the last: that of the lane before
+    const int cw = min(cv, pieces - 1) * V, c = min(cw, a.C - V), first = cw - c;  // channels before `first` are another lane's
     const size_t q = ((size_t)share * 4 + wave) * per + lane / a.lanes;  // the run
     Wide<V> dw[W], db{};
 #pragma unroll
@@ -382,7 +387,7 @@ void by_kind(la_dtype dt, la_dtype wt, la_act act, int taps, F f)
 
 la_status check(size_t stride, int B, int N, int C, int W, la_act act, la_dtype dt, la_dtype wt)
 {
-    if (B < 1 || N < 1 || C < 1 || N > 1 << 30 || W < 2 || W > kMostTaps || stride < (size_t)C) return LA_ERR_SHAPE;
+    if (B < 1 || N < 1 || C < 1 || N > 1 << 30 || C > INT_MAX - 256 || W < 2 || W > kMostTaps || stride < (size_t)C) return LA_ERR_SHAPE;
     if (!real_type(dt) || (wt != LA_F32 && wt != dt) || (act != LA_ACT_NONE && act != LA_ACT_SILU)) return LA_ERR_UNSUPPORTED;
     if ((double)B * N * (double)stride >= 1099511627776.0) return LA_ERR_SHAPE;             // 2^40
     if ((double)B * C * ((N + 15) / 16) >= 2147483648.0) return LA_ERR_SHAPE;  // runs' channels
@@ -400,7 +405,7 @@ Back back_of(int B, int N, int C, int most)
 {
     Back p;
     p.V = C < most ? 1 : most;
-    const int pieces = (C + p.V - 1) / p.V;
+    const int pieces = pieces_of(C, p.V);
     p.lanes = 1;
     while (p.lanes < 64 && p.lanes < pieces) p.lanes *= 2;
     p.columns = (pieces + p.lanes - 1) / p.lanes;
@@ -445,7 +450,7 @@ la_status la_conv_forward(const void *X, size_t x_stride, const void *Wt, const 
         constexpr int K = decltype(taps)::value, V = la::wide_of<K>;
         auto go = [&](auto wide) {
             constexpr int U = decltype(wide)::value;
-            const size_t each = (C + U - 1) / U;
+            const size_t each = la::pieces_of(C, U);
             a.run = la::run_rows(B, N, each, 4096);
             a.runs = (N + a.run - 1) / a.run;
             a.items = (size_t)B * a.runs * each;

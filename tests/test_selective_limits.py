@@ -1,4 +1,6 @@
 """Host-only checks of what the short convolution and the selective scan take and refuse at the edges of their range."""
+import ctypes
+
 import pytest
 import torch
 
@@ -43,3 +45,15 @@ def test_rows_far_apart_are_copied_for_the_scan():
     assert binding._near(near, 1, None) is near and _rows_in_place(near, 1, binding.ROWS_APART) is near
     wide = torch.empty(1, 1, 1 << 24, dtype=torch.bfloat16)  # refused, not copied
     assert binding._near(wide, 1, None) is wide and binding._near(None, 1, None) is None
+
+
+def test_channels_that_integers_would_pass_are_refused():
+    """Numbers of channels next to 2^31, where rounding up to a workgroup's would overflow."""
+    lib = la.load_library()
+    p = [ctypes.c_void_p(0x10000000 + (k << 42)) for k in range(8)]
+    for C in ((1 << 31) - 256, (1 << 31) - 64, (1 << 31) - 1):
+        assert lib.la_conv_forward(p[0], C, p[1], None, None, p[2], None, None, 1, 1, C, 2, 1, 1, 1, None) == 2
+        assert lib.la_conv_step(p[0], C, p[1], None, p[3], p[2], 1, 1, C, 2, 1, 1, 1, None) == 2
+        assert lib.la_conv_backward(p[0], C, p[1], None, None, p[2], None, p[3], p[4], None, None, None, 1, 1, C, 2, 1, 1, 1, p[5], 1 << 41, None) == 2
+        assert lib.la_conv_workspace_bytes(1, 1, C, 2) == 0
+    assert lib.la_conv_workspace_bytes(1, 1, (1 << 31) - 257, 2) == 3 * 4 * ((1 << 31) - 257) // 256 * 256 + 256
