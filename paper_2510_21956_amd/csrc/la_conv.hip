@@ -62,7 +62,7 @@ struct Conv {
     void *dX, *dstate;
     float *shares;                // [shares, W + 1, C] sums of dw and dbias
     const int *lengths;
-    size_t xs, items;
+    size_t xs, items, from;       // from: the launch's first item
     int B, N, C, run, runs, lanes, columns;
 };
 // Pieces of V channels in a row.
@@ -115,7 +115,7 @@ constexpr int rows_together = W >= 4 ? W : W == 3 ? 6 : 4;
 template <typename T, typename WT, int V, int W, int ACT>
 __global__ void __launch_bounds__(256) k_conv(Conv a)
 {
-    const size_t i = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t i = a.from + (size_t)blockIdx.x * 256 + threadIdx.x;
     const int pieces = pieces_of(a.C, V);
     if (i >= a.items) {
         const size_t k = i - a.items;
@@ -292,12 +292,12 @@ __global__ void __launch_bounds__(256) k_conv_back(Conv a)
                         (sums[0][j][lane][k] + sums[1][j][lane][k]) + (sums[2][j][lane][k] + sums[3][j][lane][k]);
 }
 
-// dw and dbias from the workgroups' shares: 64 channels a workgroup, its waves take every 16th share each.
+// dw and dbias from the workgroups' shares: 64 channels a workgroup, from c0 on, its waves take every 16th share each.
 template <int W>
-__global__ void __launch_bounds__(1024) k_conv_join(const float *shares, float *dW, float *db, int count, int C)
+__global__ void __launch_bounds__(1024) k_conv_join(const float *shares, float *dW, float *db, int count, int C, int c0)
 {
     __shared__ float sums[16][64];
-    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = blockIdx.x * 64 + lane, j = blockIdx.y;
+    const int lane = threadIdx.x % 64, wave = threadIdx.x / 64, c = c0 + blockIdx.x * 64 + lane, j = blockIdx.y;
     float s = 0.f;
     if (c < C)
         for (int k = wave; k < count; k += 16) s += shares[((size_t)k * (W + 1) + j) * C + c];
@@ -343,6 +343,8 @@ __global__ void __launch_bounds__(256) k_conv_step(Conv a)
 }
 
 constexpr int kMostTaps = 8;
+constexpr size_t kMostItems = 1u << 31;  // of a launch, whose threads are counted in 32 bits: with `last`, up to 7 * 2^31 in all
+constexpr int kMostJoined = 1 << 27;         // channels of a launch of k_conv_join, 16 threads each
 
 // Channels a lane takes: four, two where the taps would fill the registers, backward two; one where a row is shorter.  More of
 // them leave fewer waves, whose loads are not enough: 8 x 2048 rows of 2048, bf16, forward 28 us, with eight 36; backward
@@ -455,7 +457,10 @@ la_status la_conv_forward(const void *X, size_t x_stride, const void *Wt, const 
             a.runs = (N + a.run - 1) / a.run;
             a.items = (size_t)B * a.runs * each;
             const size_t all = a.items + (last ? (size_t)B * (K - 1) * each : 0);
-            la::k_conv<T, WT, U, K, decltype(act_)::value><<<dim3((unsigned)((all + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream>>>(a);
+            for (a.from = 0; a.from < all; a.from += la::kMostItems) {
+                const size_t n = all - a.from < la::kMostItems ? all - a.from : la::kMostItems;
+                la::k_conv<T, WT, U, K, decltype(act_)::value><<<dim3((unsigned)((n + 255) / 256)), dim3(256), 0, (hipStream_t)hip_stream>>>(a);
+            }
         };
         if (C >= V) go(std::integral_constant<int, V>());
         else go(std::integral_constant<int, 1>());
@@ -503,7 +508,12 @@ la_status la_conv_backward(const void *X, size_t x_stride, const void *Wt, const
         if (C < V) go(std::integral_constant<int, 1>(), few);
         else if (p.run >= la::kLongRun) go(std::integral_constant<int, V>(), many);
         else go(std::integral_constant<int, V>(), few);
-        if (need) la::k_conv_join<K><<<dim3((C + 63) / 64, K + 1), dim3(1024), 0, st>>>(a.shares, dW, dbias, p.count, C);
+        if (need)
+            for (int c0 = 0; c0 < C; c0 += la::kMostJoined) {
+                const int n = C - c0 < la::kMostJoined ? C - c0 : la::kMostJoined;
+                la::k_conv_join<K><<<dim3((n + 63) / 64, K + 1), dim3(1024), 0, st>>>(a.shares, dW, dbias, p.count, C, c0);
+                if (n < la::kMostJoined) break;
+            }
     });
     return la::done();
 }

@@ -90,3 +90,29 @@ def test_tokens_out_of_a_long_batch(monkeypatch, native, streams):
                 got.append([state, y, z, last, *grads])
             assert all(torch.equal(p, q) for p, q in zip(*got)) and torch.isfinite(got[0][1]).all()
             assert torch.equal(got[0][0], got[0][3])
+
+
+def test_more_channels_than_a_launch_has_threads():
+    """One row of 2^30 channels in all, eight taps, and the rows to carry on: 2^32 threads in two launches and more.  y is the
+    last tap's product, `last` zeros and the row itself."""
+    B, C, W = 2, 1 << 29, 8
+    x = torch.randn(B, 1, C, dtype=torch.bfloat16, device="cuda")
+    w = torch.ones(C, W, dtype=torch.bfloat16, device="cuda")
+    y = poison(B, 1, C, dtype=x.dtype)
+    last = poison(B, W - 1, C, dtype=x.dtype)
+    la.la_conv_forward(x, w, None, None, y, last, None, la.LA_ACT_NONE)
+    assert torch.equal(y, x)
+    for b in range(B):
+        assert torch.equal(last[b, -1], x[b, 0])
+        for j in range(W - 2):
+            assert not last[b, j].any()
+
+
+def test_sums_of_more_channels_than_a_launch_has():
+    """dw and dbias of 2^28 channels and some more: one row's, dy x and dy."""
+    C = (1 << 28) + 65
+    x, dy = torch.randn(1, 1, C, device="cuda"), torch.randn(1, 1, C, device="cuda")
+    w = torch.ones(C, 2, device="cuda")
+    dx, dw, db = poison(1, 1, C), poison(C, 2), poison(C)
+    la.la_conv_backward(x, w, None, None, dy, None, dx, dw, db, None, None, la.LA_ACT_NONE, room(la.la_conv_workspace_bytes(1, 1, C, 2)))
+    assert torch.equal(dx, dy) and torch.equal(db, dy[0, 0]) and torch.equal(dw[:, 1], (x * dy)[0, 0]) and not dw[:, 0].any()
