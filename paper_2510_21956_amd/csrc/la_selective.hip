@@ -444,6 +444,9 @@ __device__ __forceinline__ float4 over_lanes(float (&v)[64])
             : "+v"(v[i]), "+v"(v[i + 1]), "+v"(v[i + 2]), "+v"(v[i + 3])
             : "v"(v[i + 16]), "v"(v[i + 17]), "v"(v[i + 18]), "v"(v[i + 19]));
 #pragma unroll
+    for (int i = 0; i < 8; i += 4)  // the compiler does not see what the instructions above wrote: it would not wait
+        asm("s_nop 1" : "+v"(v[i]), "+v"(v[i + 1]), "+v"(v[i + 2]), "+v"(v[i + 3]), "+v"(v[i + 8]), "+v"(v[i + 9]), "+v"(v[i + 10]), "+v"(v[i + 11]));
+#pragma unroll
     for (int i = 0; i < 8; ++i) {
         const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[i]), __float_as_uint(v[i + 8]), false, false);
         v[i] = __uint_as_float(s[0]) + __uint_as_float(s[1]);

@@ -1,5 +1,9 @@
 """Host-only checks of what the short convolution and the selective scan take and refuse at the edges of their range."""
 import ctypes
+import os
+import re
+import struct
+import subprocess
 
 import pytest
 import torch
@@ -57,3 +61,55 @@ def test_channels_that_integers_would_pass_are_refused():
         assert lib.la_conv_backward(p[0], C, p[1], None, None, p[2], None, p[3], p[4], None, None, None, 1, 1, C, 2, 1, 1, 1, p[5], 1 << 41, None) == 2
         assert lib.la_conv_workspace_bytes(1, 1, C, 2) == 0
     assert lib.la_conv_workspace_bytes(1, 1, (1 << 31) - 257, 2) == 3 * 4 * ((1 << 31) - 257) // 256 * 256 + 256
+
+
+def _device_code(path):
+    """The code objects for the GPU inside a library: bundles of a count, then offset, size and name of each."""
+    data, at, magic = open(path, "rb").read(), 0, b"__CLANG_OFFLOAD_BUNDLE__"
+    while (at := data.find(magic, at)) >= 0:
+        here = at + 24
+        count, = struct.unpack_from("<Q", data, here)
+        here += 8
+        for _ in range(count if count < 16 else 0):
+            offset, size, n = struct.unpack_from("<3Q", data, here)
+            if data[here + 24:here + 24 + n].startswith(b"hip") and size:
+                yield data[at + offset:at + offset + size]
+            here += 24 + n
+        at += 24
+
+
+def _registers(operand):
+    m = re.match(r"-?\|?v(\d+)$|-?\|?v\[(\d+):(\d+)\]$", operand.strip().rstrip("|"))
+    return range(0) if not m else range(int(m[1]), int(m[1]) + 1) if m[1] else range(int(m[2]), int(m[3]) + 1)
+
+
+def test_other_lanes_registers_are_waited_for(tmp_path):
+    """In the scan's kernels as they are built: two instructions, or a wait as long, between what writes a register and what reads
+    another lane's place of it (DPP forms, swaps of halves and quarters); the compiler does not see into inline assembly."""
+    tool = "/opt/rocm/llvm/bin/llvm-objdump"
+    if not os.path.exists(tool):
+        pytest.skip("no disassembler")
+    la.load_library()
+    code = [c for c in _device_code(binding.library_path()) if b"k_selective_back" in c]
+    assert len(code) == 1
+    (tmp_path / "code.o").write_bytes(code[0])
+    text = subprocess.run([tool, "-d", "--no-show-raw-insn", str(tmp_path / "code.o")], check=True, capture_output=True, text=True).stdout
+    written, now, seen = {}, 0, 0
+    for line in text.splitlines():
+        m = re.match(r"\s+(\w+)\s*([^/]*)", line)
+        if not m:
+            written = {}  # another function, or a label
+            continue
+        op, operands = m[1], m[2].split(",")
+        now += 1
+        swap = op.startswith("v_permlane") and "swap" in op
+        if swap or op.endswith("_dpp") or " row_" in m[2] or "quad_perm" in m[2]:
+            seen += 1
+            for r in [*_registers(operands[0]), *_registers(operands[1])] if swap else _registers(operands[1].split(" ")[1]):
+                assert now - written.get(r, -9) > 2, line
+        if op == "s_nop":
+            now += int(operands[0], 0)
+        elif op.startswith("v_"):
+            for r in [*_registers(operands[0]), *(_registers(operands[1]) if swap else ())]:
+                written[r] = now
+    assert seen > 10000
