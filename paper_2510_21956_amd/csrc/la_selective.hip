@@ -213,15 +213,29 @@ __device__ __forceinline__ float decay_of(float A)
     const float x = A * kLog2e, low = -0x1.fffffep127f;
     return x < low ? low : x;
 }
+// (Places behind the last state have its decay: a number wherever that is one.)
 template <int P>
 __device__ __forceinline__ void decays(const Scan &a, const Spot &p, int wave, float (&A)[P])
 {
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-        const int s = wave * P + j;
-        A[j] = s < a.S ? decay_of(a.A[(size_t)p.c * a.S + s]) : 0.f;
+        A[j] = decay_of(a.A[(size_t)p.c * a.S + min(wave * P + j, a.S - 1)]);
     }
 }
+// v, or 0 where the mask is 0, also of an infinity.
+__device__ __forceinline__ float held(float v, uint32_t mask) { return __uint_as_float(__float_as_uint(v) & mask); }
+// Which of a wave's places hold a state: the others have B = 0 and C = 0, and what would be an infinity times these is taken out.
+// FILLED: all do.
+template <int P, bool FILLED>
+struct Places {
+    uint32_t mask[P];
+    __device__ __forceinline__ Places(const Scan &a, int wave)
+    {
+#pragma unroll
+        for (int j = 0; j < P; ++j) mask[j] = wave * P + j < a.S ? 0xffffffffu : 0;
+    }
+    __device__ __forceinline__ float of(float v, int j) const { return FILLED ? v : held(v, mask[j]); }
+};
 // The states that the walk starts from: the caller's, or those that k_selective_chain left for the segment.
 template <int P>
 __device__ __forceinline__ void states_from(const Scan &a, const Spot &p, int wave, float (&h)[P])
@@ -298,7 +312,7 @@ __global__ void __launch_bounds__(256) k_selective_chain(Scan a)
 }
 
 // FULL: outputs.  Else what the segment makes of zero states.
-template <typename T, int P, int W, bool FULL>
+template <typename T, int P, int W, bool FULL, bool FILLED>
 __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
 {
     constexpr int OWN = (kPairs + W - 1) / W;  // pairs of rows that a wave prepares
@@ -306,6 +320,7 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
     __shared__ float2 ys[FULL ? W : 1][kPairs][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Spot p(a, lane);
+    const Places<P, FILLED> places(a, wave);
     float A[P], h[P];
     Span span;
     decays<P>(a, p, wave, A);
@@ -381,7 +396,8 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
             each<2>([&](auto r_) {
                 constexpr int r = decltype(r_)::value, k = (2 * q + r) * P;
                 each<P>([&](auto j) {
-                    h[j] = fmaf(f[r * P + j], h[j], (r ? s.w : s.y) * of_lane<k % 16 + decltype(j)::value>(B.v[k / 16]));
+                    const float u = places.of(r ? s.w : s.y, j);
+                    h[j] = fmaf(f[r * P + j], h[j], u * of_lane<k % 16 + decltype(j)::value>(B.v[k / 16]));
                 });
                 if (FULL) y[r] = sum_all<k % 16>(C.v[k / 16], h);
             });
@@ -467,7 +483,7 @@ __device__ __forceinline__ float4 over_lanes(float (&v)[64])
 // Registers, of as many waves to a SIMD as the attribute says: 168 for three (four or six waves a workgroup spill 16 to 20 bytes a
 // lane, for 170 and two waves they would not); eight waves, of which four to a SIMD would have 128 and spill 136 bytes, run
 // two to a SIMD (4 x 2048 rows of 1024, 32 states, fp32: 280 us, with four 379); 16 waves a workgroup can't have more than 128.
-template <typename T, int P, int W, bool FULL>
+template <typename T, int P, int W, bool FULL, bool FILLED>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FULL || W == 16 ? 4 : W == 8 ? 2 : 3))) k_selective_back(Scan a)
 {
     constexpr int OWN = (kPairs + W - 1) / W, PART = kCells / P, PARTS = kRows / PART;
@@ -476,6 +492,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
     __shared__ float4 gs[FULL ? W : 1][kPairs][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Spot p(a, lane);
+    const Places<P, FILLED> places(a, wave);
     float A[P], carry[P], dA[P], before[P], dD = 0.f, db = 0.f;
     Span span;
     decays<P>(a, p, wave, A);
@@ -513,7 +530,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
     };
     // lanes without a channel of their own have no share in the sums over channels
     const uint32_t mask = p.live ? 0xffffffffu : 0;
-    auto of_live = [&](float v) { return __uint_as_float(__float_as_uint(v) & mask); };
+    auto of_live = [&](float v) { return held(v, mask); };
     if (tiles) request(p.r1 - last);
     for (int k = 0, rows = p.r1 - last; k < tiles; ++k, rows = kRows) {
         float xw[OWN][2], slope[OWN][2];
@@ -555,7 +572,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
                     const float4 s = du[q][lane];
                     each<2 * P>([&](auto i) {
                         constexpr int r = decltype(i)::value / P, j = decltype(i)::value % P, k = (2 * q + r) * P + j;
-                        h0[j] = fmaf(__builtin_amdgcn_exp2f((r ? s.z : s.x) * A[j]), h0[j], (r ? s.w : s.y) * of_lane<k % 16>(B.v[k / 16]));
+                        const float u = places.of(r ? s.w : s.y, j);
+                        h0[j] = fmaf(__builtin_amdgcn_exp2f((r ? s.z : s.x) * A[j]), h0[j], u * of_lane<k % 16>(B.v[k / 16]));
                     });
                     if (q % 2) keep_order();
                 });
@@ -565,8 +583,9 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
                     const float4 next = du[first + (q + 1 < PART / 2 ? q + 1 : q)][lane];
                     each<2 * P>([&](auto i) {
                         constexpr int r = decltype(i)::value / P, j = decltype(i)::value % P, k = (2 * q + r) * P + j, at = k + 2 * first * P;
+                        const float u = places.of(r ? s.w : s.y, j);
                         f[k] = __builtin_amdgcn_exp2f((r ? s.z : s.x) * A[j]);
-                        h[k] = fmaf(f[k], k >= P ? h[k - P] : h0[j], (r ? s.w : s.y) * of_lane<at % 16>(B.v[at / 16]));
+                        h[k] = fmaf(f[k], k >= P ? h[k - P] : h0[j], u * of_lane<at % 16>(B.v[at / 16]));
                         settle(f[k]), settle(h[k]);
                     });
                     s = next;
@@ -582,6 +601,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
                         constexpr int r = 1 - decltype(r_)::value, k = (2 * q + r) * P, at = k + 2 * first * P;
                         const float d = r ? s.z : s.x, u = r ? s.w : s.y, y = r ? y2.y : y2.x;
                         fma_each<at % 16>(carry, C.v[at / 16], y);
+#pragma unroll
+                        for (int j = 0; j < P; ++j) carry[j] = places.of(carry[j], j);
                         gu[r] = sum_all<at % 16>(B.v[at / 16], carry);
 #pragma unroll
                         for (int j = 0; j < P; ++j) {
@@ -758,7 +779,7 @@ __global__ void __launch_bounds__(256) k_selective_step(Scan a, float *state, in
 #pragma unroll
     for (int j = 0; j < P; ++j) {
         const int s = l * P + j;
-        A[j] = s < a.S ? decay_of(a.A[(size_t)c * a.S + s]) : 0.f;
+        A[j] = decay_of(a.A[(size_t)c * a.S + min(s, a.S - 1)]);
         h[j] = s < a.S ? state[k * a.S + s] : 0.f;
     }
     const float bias = a.bias ? a.bias[c] : 0.f, D = a.D ? a.D[c] : 0.f;
@@ -773,7 +794,7 @@ __global__ void __launch_bounds__(256) k_selective_step(Scan a, float *state, in
             const int s = l * P + j;
             const float Bt = s < a.S ? load_elem((const T *)a.Bm, row * a.bs + g * a.S + s) : 0.f;
             const float Ct = s < a.S ? load_elem((const T *)a.Cm, row * a.cs + g * a.S + s) : 0.f;
-            h[j] = fmaf(__builtin_amdgcn_exp2f(d * A[j]), h[j], u * Bt);
+            h[j] = fmaf(__builtin_amdgcn_exp2f(d * A[j]), h[j], s < a.S ? u * Bt : 0.f);
             y = fmaf(Ct, h[j], y);
         }
         for (int m = 1; m < L; m *= 2) y += __shfl_xor(y, m);
@@ -985,11 +1006,12 @@ la_status la_selective_forward(const void *X, size_t x_stride, const void *Dt, s
         constexpr int p = decltype(P)::value, w = decltype(W)::value;
         if constexpr (p > 2 || w <= 4) {  // (else two states a wave of one piece: lay_out)
             if (a.segs > 1) {
-                la::k_selective<T, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective<T, p, w, false, true><<<grid, dim3(64 * w), 0, st>>>(a);
                 la::k_selective_chain<false><<<chain, dim3(256), 0, st>>>(a);
             }
         }
-        la::k_selective<T, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
+        if (S == p * w) la::k_selective<T, p, w, true, true><<<grid, dim3(64 * w), 0, st>>>(a);
+        else la::k_selective<T, p, w, true, false><<<grid, dim3(64 * w), 0, st>>>(a);
     };
     la::by_shape<false>(shape, [&](auto P, auto W) {
         if (dt == LA_F32) run((float *)nullptr, P, W);
@@ -1036,11 +1058,12 @@ la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, 
         constexpr int p = decltype(P)::value, w = decltype(W)::value;
         if constexpr (p > 2 || w <= 4) {
             if (a.segs > 1) {
-                la::k_selective_back<T, p, w, false><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective_back<T, p, w, false, true><<<grid, dim3(64 * w), 0, st>>>(a);
                 la::k_selective_chain<true><<<chain, dim3(256), 0, st>>>(a);
             }
         }
-        la::k_selective_back<T, p, w, true><<<grid, dim3(64 * w), 0, st>>>(a);
+        if (S == p * w) la::k_selective_back<T, p, w, true, true><<<grid, dim3(64 * w), 0, st>>>(a);
+        else la::k_selective_back<T, p, w, true, false><<<grid, dim3(64 * w), 0, st>>>(a);
     };
     la::by_shape<true>(shape, [&](auto P, auto W) {
         if (dt == LA_F32) run((float *)nullptr, P, W);

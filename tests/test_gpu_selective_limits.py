@@ -1,11 +1,14 @@
 """The short convolution and the selective scan where their tests against the definition do not go: long segments, layouts of many
 chains, infinities, rows that lie far apart."""
+import math
+
 import pytest
 import torch
 
 import paper_2510_21956_amd as la
 from layer_reference import U
 from paper_2510_21956_amd import binding
+from selective_reference import Scan64
 
 pytestmark = pytest.mark.gpu
 F = torch.float32
@@ -116,3 +119,55 @@ def test_sums_of_more_channels_than_a_launch_has():
     dx, dw, db = poison(1, 1, C), poison(C, 2), poison(C)
     la.la_conv_backward(x, w, None, None, dy, None, dx, dw, db, None, None, la.LA_ACT_NONE, room(la.la_conv_workspace_bytes(1, 1, C, 2)))
     assert torch.equal(dx, dy) and torch.equal(db, dy[0, 0]) and torch.equal(dw[:, 1], (x * dy)[0, 0]) and not dw[:, 0].any()
+
+
+def as_defined(got, want, off, name):
+    """NaN where the definition has NaN, infinities where it has them, what is finite within its bounds (where infinities spoil a
+    bound, nothing is asked)."""
+    got, want = got.cpu().double(), want.double()
+    assert torch.equal(got.isnan(), want.isnan()), (name, "NaN", int(got.isnan().sum()), int(want.isnan().sum()))
+    assert torch.equal(got == math.inf, want == math.inf) and torch.equal(got == -math.inf, want == -math.inf), name
+    known = want.isfinite() & off.isfinite()
+    assert ((got - want).abs() <= off + U * want.abs())[known].all(), name
+
+
+INFINITE = ["x", "last x", "dt", "B", "C", "h0", "dy", "dlast"]
+# places behind the last state: one piece and segments, few sequences and many
+PLACES = [(2, 32, 64, 1, 1), (2, 32, 64, 3, 1), (1, 32, 64, 5, 1), (1, 48, 64, 9, 1), (1, 32, 64, 13, 1), (1, 32, 128, 20, 2), (1, 320, 64, 20, 1),
+          (1, 32, 64, 40, 1), (1, 16, 64, 50, 1), (1, 16, 64, 70, 1), (1, 16, 64, 100, 1), (260, 16, 64, 14, 1)]
+
+
+@pytest.mark.parametrize("what", INFINITE)
+@pytest.mark.parametrize("B,N,C,S,G", PLACES)
+def test_infinities_are_those_of_the_definition(B, N, C, S, G, what):
+    """One infinite value.  Everything else is positive, so that sums over states keep the infinity's sign: what has no value of its
+    own, places behind the last state, lanes behind the last channel, rows behind a tile's last, must not turn it into NaN."""
+    gen = torch.Generator().manual_seed(N + C + S)
+    r = lambda *s: torch.rand(*s, generator=gen) + 0.5  # noqa: E731
+    x, dt, A, Bm, Cm, D = r(B, N, C), r(B, N, C) / 8, -r(C, S) / 4, r(B, N, G, S), r(B, N, G, S), r(C)
+    h0, dy, dlast, step = r(B, C, S), r(B, N, C), r(B, C, S), "value"
+    at = {"x": (x, N // 2), "last x": (x, N - 1), "dt": (dt, N // 2), "B": (Bm, N // 2), "C": (Cm, N // 2), "dy": (dy, N // 2)}
+    if what in at:
+        t, row = at[what]
+        t[B - 1, row].view(-1)[-1] = math.inf
+    else:
+        (h0 if what == "h0" else dlast)[B - 1, C - 1, S - 1] = math.inf
+    ref = Scan64(x[-1:], dt[-1:], A, Bm[-1:], Cm[-1:], D, None, h0[-1:], None, step)
+    dev = [t.cuda() for t in (x, dt, A, Bm, Cm, D)]
+    y, last, saved = poison(B, N, C), poison(B, C, S), room(la.la_selective_saved_bytes(B, N, C, S))
+    la.la_selective_forward(*dev, None, h0.cuda(), y, last, saved, None, la.LA_STEP_VALUE, room(la.la_selective_workspace_bytes(B, N, C, S, G, 0)))
+    as_defined(y[-1:], ref.y, ref.Ey, "y")
+    as_defined(last[-1:], ref.last, ref.Elast, "last")
+    state, z = h0.cuda(), poison(B, N, C)
+    la.la_selective_step(*dev, None, state, z, la.LA_STEP_VALUE)
+    as_defined(z[-1:], ref.y, ref.Ey, "y in steps")
+    as_defined(state[-1:], ref.last, ref.Elast, "state in steps")
+    out = [poison(*s) for s in ((B, N, C), (B, N, C), (C, S), Bm.shape, Bm.shape, (C,), (C,), (B, C, S))]
+    la.la_selective_backward(*dev, None, saved, dy.cuda(), dlast.cuda(), *out, None, la.LA_STEP_VALUE,
+                             room(la.la_selective_workspace_bytes(B, N, C, S, G, 1)))
+    want, off = ref.backward(dy[-1:], dlast[-1:])
+    for k, got in zip(("x", "dt", "A", "B", "C", "D", "bias", "h0"), out):
+        if got.shape[0] == B and got.dim() > 1 and k != "A":
+            as_defined(got[-1:], want[k], off[k], "d" + k)
+        elif B == 1:
+            as_defined(got, want[k], off[k], "d" + k)
