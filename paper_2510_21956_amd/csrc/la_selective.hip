@@ -541,7 +541,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
             float d[2], y[2];
 #pragma unroll
             for (int r = 0; r < 2; ++r) {
-                d[r] = step_of<sizeof(T) == 4>(load_elem(dt[i], r) + bias, a.step, slope[i][r]);
+                d[r] = of_live(step_of<sizeof(T) == 4>(load_elem(dt[i], r) + bias, a.step, slope[i][r]));
                 xw[i][r] = FULL ? of_live(load_elem(x[i], r)) : 0.f;
                 y[r] = of_live(load_elem(dy[i], r));
                 if (2 * q + r >= rows) d[r] = xw[i][r] = y[r] = 0.f;
@@ -622,6 +622,10 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
                 });
 #pragma unroll
                 for (int j = 0; j < P; ++j) dA[j] += own[j];
+                // lanes without a channel: B or C may be infinite.  Columns that have none skip this.
+                if (!p.live)
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) asm volatile("v_mov_b32 %0, 0" : "=v"(v[i]));
                 const float4 sum = over_lanes(v);
                 if (lane % 4 == 0)
                     *(float4 *)(shares + part * 64 + (lane & 8) * 4 + (lane & 4) * 4 + (lane & 32) / 4 + (lane & 16) / 4) = sum;

@@ -135,10 +135,13 @@ INFINITE = ["x", "last x", "dt", "B", "C", "h0", "dy", "dlast"]
 # places behind the last state: one piece and segments, few sequences and many
 PLACES = [(2, 32, 64, 1, 1), (2, 32, 64, 3, 1), (1, 32, 64, 5, 1), (1, 48, 64, 9, 1), (1, 32, 64, 13, 1), (1, 32, 128, 20, 2), (1, 320, 64, 20, 1),
           (1, 32, 64, 40, 1), (1, 16, 64, 50, 1), (1, 16, 64, 70, 1), (1, 16, 64, 100, 1), (260, 16, 64, 14, 1)]
+# lanes behind the last channel
+LANES = [(2, 32, 5, 2, 1), (2, 32, 70, 3, 1), (1, 32, 66, 8, 2), (1, 48, 70, 16, 1), (1, 32, 130, 20, 2), (1, 304, 8, 20, 1), (300, 16, 8, 14, 1), (1, 16, 66, 64, 1),
+         (1, 16, 66, 128, 1), (2, 192, 8, 100, 1)]
 
 
 @pytest.mark.parametrize("what", INFINITE)
-@pytest.mark.parametrize("B,N,C,S,G", PLACES)
+@pytest.mark.parametrize("B,N,C,S,G", PLACES + LANES)
 def test_infinities_are_those_of_the_definition(B, N, C, S, G, what):
     """One infinite value.  Everything else is positive, so that sums over states keep the infinity's sign: what has no value of its
     own, places behind the last state, lanes behind the last channel, rows behind a tile's last, must not turn it into NaN."""
