@@ -306,7 +306,8 @@ __global__ void __launch_bounds__(256) k_selective_chain(Scan a)
             if (k0 + i >= a.segs) break;
             const size_t at = (size_t)b * a.segs + (BWD ? a.segs - 1 - k0 - i : k0 + i);
             a.sums[(at * a.S + s) * a.C + c] = h;
-            h = fmaf(__builtin_amdgcn_exp2f(span[i] * A), h, own[i]);
+            const float f = __builtin_amdgcn_exp2f(span[i] * A);  // 0 behind many rows, of which none had 0
+            h = fabsf(h) == INFINITY && f == 0.f ? h + own[i] : fmaf(f, h, own[i]);
         }
     }
 }

@@ -174,3 +174,18 @@ def test_infinities_are_those_of_the_definition(B, N, C, S, G, what):
             as_defined(got[-1:], want[k], off[k], "d" + k)
         elif B == 1:
             as_defined(got, want[k], off[k], "d" + k)
+
+
+@pytest.mark.parametrize("S", [5, 16, 20])
+def test_an_infinite_state_through_many_segments(S):
+    """A state that is infinite stays so, however little the decays of a segment's rows leave together: exp(-5) a row."""
+    N, C = 4000, 8
+    ones = lambda *s: torch.ones(*s, device="cuda")  # noqa: E731
+    x, A, Bm, h0 = ones(1, N, C), -ones(C, S), ones(1, N, S), ones(1, C, S)
+    h0[0, 3, 1] = math.inf
+    y, last = poison(1, N, C), poison(1, C, S)
+    la.la_selective_forward(x, 5 * x, A, Bm, Bm, None, None, h0, y, last, None, None, la.LA_STEP_VALUE,
+                            room(la.la_selective_workspace_bytes(1, N, C, S, 1, 0)))
+    assert (y[0, :, 3] == math.inf).all() and last[0, 3, 1] == math.inf
+    rest = [c for c in range(C) if c != 3]
+    assert torch.isfinite(y[0, :, rest]).all() and int(torch.isfinite(last).sum()) == C * S - 1
