@@ -49,6 +49,10 @@ struct Scan {
     int step;
 };
 
+__device__ __forceinline__ int rows_of(const Scan &a, int b)
+{
+    return a.lengths ? min(max(a.lengths[b], 0), a.N) : a.N;
+}
 // Where a workgroup is: its sequence, channels and rows.
 struct Spot {
     int b, column, g, seg, n, r0, r1;
@@ -717,7 +721,7 @@ __global__ void __launch_bounds__(256) k_selective_shares(Scan a, T *dB, T *dC, 
         const int tile = (int)(k % a.tiles), g = (int)(k / a.tiles % a.G), b = (int)(k / a.tiles / a.G);
         const int t = tile * kRows + v / 64 % parts * part + m / P, s = w * P + m % P;
         if (t >= a.N || s >= a.S) continue;
-        const int n = a.lengths ? min(max(a.lengths[b], 0), a.N) : a.N;
+        const int n = rows_of(a, b);
         float sum = 0.f;
         if (t < n) {
             const size_t step = (size_t)a.tiles * each;
@@ -736,8 +740,36 @@ __global__ void __launch_bounds__(256) k_selective_shares(Scan a, T *dB, T *dC, 
     }
 }
 
+// dA of the rows [r0, n) of a sequence's last segment, one at a time, as far as it is a number.  The walk gives the rows that the last tile
+// has room for behind them d = 0, which leaves nothing of these in the sums but where the state there or its gradient is not finite.
+template <typename T>
+__device__ float sum_of_rows(const Scan &a, int b, int r0, int n, int s, int c)
+{
+    const int g = c / a.group;
+    const float A = decay_of(a.A[(size_t)c * a.S + s]), bias = a.bias ? a.bias[c] : 0.f;
+    auto step = [&](size_t row) {
+        float slope;
+        return step_of<sizeof(T) == 4>(load_elem((const T *)a.Dt, row * a.ts + c) + bias, a.step, slope);
+    };
+    float carry = a.segs > 1 ? a.sums[(((size_t)b * a.segs + r0 / a.seg) * a.S + s) * a.C + c] : a.first ? a.first[((size_t)b * a.C + c) * a.S + s] : 0.f;
+    float sum = 0.f;
+    for (int t = n - 1; t >= r0 && sum == sum; --t) {
+        const size_t row0 = (size_t)b * a.N, row = row0 + t;
+        float h = a.saved[(((size_t)b * a.tiles + t / kRows) * a.S + s) * a.C + c];  // before row t, from the tile's first on
+        for (size_t k = row0 + t / kRows * kRows; k < row; ++k) {
+            const float d = step(k), u = d * load_elem((const T *)a.X, k * a.xs + c);
+            h = fmaf(__builtin_amdgcn_exp2f(d * A), h, u * load_elem((const T *)a.Bm, k * a.bs + g * a.S + s));
+        }
+        const float d = step(row), C = load_elem((const T *)a.Cm, row * a.cs + g * a.S + s);
+        carry = fmaf(C, load_elem((const T *)a.dY, row * a.C + c), carry) * __builtin_amdgcn_exp2f(d * A);
+        sum = fmaf(carry * h, d, sum);
+    }
+    return sum;
+}
+
 // dA, dD and dbias from the segments' sums: 64 channels and one row of the sums a workgroup, its waves take every 16th
 // segment each, eight of them asked for together.
+template <typename T>
 __global__ void __launch_bounds__(1024) k_selective_join(Scan a, float *dA, float *dD, float *db)
 {
     __shared__ float sums[16][64];
@@ -758,6 +790,15 @@ __global__ void __launch_bounds__(1024) k_selective_join(Scan a, float *dA, floa
             for (int i = 0; i < 8; ++i) sum += x[i];
         }
         for (; k < count; k += 16) sum += from[(size_t)k * step + c];
+        if (sum != sum && s < a.S) {  // once more, with those that rows behind a sequence may have spoilt by themselves
+            sum = 0.f;
+            for (k = wave; k < count; k += 16) {
+                const int b = k / a.segs, r0 = k % a.segs * a.seg, n = rows_of(a, b);
+                float x = from[(size_t)k * step + c];
+                if (x != x && n % kRows && n > r0 && n - r0 <= a.seg) x = sum_of_rows<T>(a, b, r0, n, s, c);
+                sum += x;
+            }
+        }
     }
     sums[wave][lane] = sum;
     block_sync();
@@ -1077,7 +1118,10 @@ la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, 
     const dim3 all = la::blocks_of((size_t)B * G * a.tiles * la::shares_of(shape));
     if (dt == LA_F32) la::k_selective_shares<float><<<all, dim3(256), 0, st>>>(a, (float *)dBm, (float *)dCm, shape.P, shape.W);
     else la::k_selective_shares<la::bf16_t><<<all, dim3(256), 0, st>>>(a, (la::bf16_t *)dBm, (la::bf16_t *)dCm, shape.P, shape.W);
-    if (dA || dD || dbias) la::k_selective_join<<<dim3((C + 63) / 64, S + 2), dim3(1024), 0, st>>>(a, dA, dD, dbias);
+    const dim3 joined((C + 63) / 64, S + 2);
+    if (!dA && !dD && !dbias) return la::done();
+    if (dt == LA_F32) la::k_selective_join<float><<<joined, dim3(1024), 0, st>>>(a, dA, dD, dbias);
+    else la::k_selective_join<la::bf16_t><<<joined, dim3(1024), 0, st>>>(a, dA, dD, dbias);
     return la::done();
 }
 

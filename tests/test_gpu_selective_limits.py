@@ -138,10 +138,13 @@ PLACES = [(2, 32, 64, 1, 1), (2, 32, 64, 3, 1), (1, 32, 64, 5, 1), (1, 48, 64, 9
 # lanes behind the last channel
 LANES = [(2, 32, 5, 2, 1), (2, 32, 70, 3, 1), (1, 32, 66, 8, 2), (1, 48, 70, 16, 1), (1, 32, 130, 20, 2), (1, 304, 8, 20, 1), (300, 16, 8, 14, 1), (1, 16, 66, 64, 1),
          (1, 16, 66, 128, 1), (2, 192, 8, 100, 1)]
+# rows behind a tile's last
+ROWS = [(2, 40, 5, 1, 1), (2, 40, 70, 3, 1), (1, 19, 64, 5, 1), (1, 37, 66, 8, 2), (1, 40, 64, 9, 1), (1, 24, 64, 13, 1), (1, 33, 70, 16, 1), (1, 40, 130, 20, 2),
+        (1, 300, 8, 20, 1), (1, 21, 64, 40, 1), (1, 21, 64, 50, 1), (1, 21, 66, 64, 1), (1, 19, 64, 70, 1), (1, 19, 66, 128, 1), (1, 211, 8, 100, 1)]
 
 
 @pytest.mark.parametrize("what", INFINITE)
-@pytest.mark.parametrize("B,N,C,S,G", PLACES + LANES)
+@pytest.mark.parametrize("B,N,C,S,G", PLACES + LANES + ROWS)
 def test_infinities_are_those_of_the_definition(B, N, C, S, G, what):
     """One infinite value.  Everything else is positive, so that sums over states keep the infinity's sign: what has no value of its
     own, places behind the last state, lanes behind the last channel, rows behind a tile's last, must not turn it into NaN."""
