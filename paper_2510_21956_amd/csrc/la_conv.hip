@@ -205,6 +205,12 @@ __global__ void __launch_bounds__(256) k_conv_back(Conv a)
         const int from = n - (W - 1);  // the first row that is carried on
         const T *Xt = X + (size_t)(t0 + U) * a.xs, *dYt = dY + (size_t)(t0 + U) * a.C;  // rows asked for next
         T *dXt = dX + (ptrdiff_t)(t0 - (W - 1)) * a.C;
+        bool endless = false;  // a tap of the wave's is infinite, or NaN: 0 times that is not 0
+#pragma unroll
+        for (int j = 0; j < W; ++j)
+#pragma unroll
+            for (int q = 0; q < V; ++q) endless = endless || !(fabsf(taps.w[j].x[q]) < INFINITY);
+        endless = __any(endless);
         // PLAIN: all rows of the turn are the run's own, and so is what they complete and ask for
         auto turn = [&](int t1, auto plain_) {
             constexpr bool PLAIN = decltype(plain_)::value;
@@ -250,6 +256,14 @@ __global__ void __launch_bounds__(256) k_conv_back(Conv a)
                 for (int j = 0; j < W; ++j)
 #pragma unroll
                     for (int q = 0; q < V; ++q) d.x[q] = fmaf(taps.w[W - 1 - j].x[q], e[(k + j) % W].x[q], d.x[q]);
+                if (!PLAIN && endless) {  // without the products with rows that there are not
+                    d = Wide<V>{};
+#pragma unroll
+                    for (int j = 0; j < W; ++j)
+#pragma unroll
+                        for (int q = 0; q < V; ++q)
+                            if (s + j >= 0 && s + j < n) d.x[q] = fmaf(taps.w[W - 1 - j].x[q], e[(k + j) % W].x[q], d.x[q]);
+                }
                 if (!PLAIN && a.dlast && s >= from && s < n) {
                     const Wide<V> l = widened(fetch<T, V>((const T *)a.dlast + ((size_t)b * (W - 1) + s - from) * a.C + c));
 #pragma unroll

@@ -8,7 +8,7 @@ import torch
 import paper_2510_21956_amd as la
 from layer_reference import U
 from paper_2510_21956_amd import binding
-from selective_reference import Scan64
+from selective_reference import Scan64, conv_backward64
 
 pytestmark = pytest.mark.gpu
 F = torch.float32
@@ -192,3 +192,28 @@ def test_an_infinite_state_through_many_segments(S):
     assert (y[0, :, 3] == math.inf).all() and last[0, 3, 1] == math.inf
     rest = [c for c in range(C) if c != 3]
     assert torch.isfinite(y[0, :, rest]).all() and int(torch.isfinite(last).sum()) == C * S - 1
+
+
+@pytest.mark.parametrize("dtype", [F, torch.bfloat16])
+@pytest.mark.parametrize("W", [2, 3, 4, 8])
+@pytest.mark.parametrize("value", [math.inf, math.nan])
+def test_weights_that_are_no_numbers_leave_padding_alone(W, dtype, value):
+    """An infinite tap or one that is NaN reaches the gradients of the rows that it has a share in: padding stays zero, and of a sequence without rows
+    the carried rows' gradient is what comes back."""
+    N, C = 70, 9
+    gen = torch.Generator().manual_seed(W)
+    r = lambda *s: torch.rand(*s, generator=gen).to(dtype) + 0.5  # noqa: E731
+    lengths = torch.tensor([N, 0, 1, 5, 33, 64], dtype=torch.int32)
+    B = len(lengths)
+    x, state, dy, dlast, w = r(B, N, C), r(B, W - 1, C), r(B, N, C), r(B, W - 1, C), r(C, W).float()
+    w[2, 0] = w[4, W - 1] = w[6, W // 2] = value
+    out = [poison(B, N, C, dtype=dtype), poison(C, W), poison(C), poison(B, W - 1, C, dtype=dtype)]
+    la.la_conv_backward(*(t.cuda() for t in (x, w)), None, *(t.cuda() for t in (state, dy, dlast)), *out, lengths.cuda(), la.LA_ACT_NONE,
+                        room(la.la_conv_workspace_bytes(B, N, C, W)))
+    want, off = conv_backward64(x, w, None, state, dy, dlast, lengths, "none")
+    half = 0 if dtype == F else 2.0 ** -8
+    for k, got, a, e in zip(("dx", "dw", "dbias", "dstate"), out, want, off):
+        as_defined(got, a, e + (half * a.abs() if k in ("dx", "dstate") else 0), k)
+    for b, n in enumerate(lengths.tolist()):
+        assert not out[0][b, n:].any()
+    assert torch.equal(out[3][1].cpu(), dlast[1])
