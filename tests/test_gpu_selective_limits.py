@@ -9,6 +9,7 @@ import paper_2510_21956_amd as la
 from layer_reference import U
 from paper_2510_21956_amd import binding
 from selective_reference import Scan64, conv_backward64
+from test_gpu_selective import check, draw
 
 pytestmark = pytest.mark.gpu
 F = torch.float32
@@ -217,3 +218,74 @@ def test_weights_that_are_no_numbers_leave_padding_alone(W, dtype, value):
     for b, n in enumerate(lengths.tolist()):
         assert not out[0][b, n:].any()
     assert torch.equal(out[3][1].cpu(), dlast[1])
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("B,N,C,S", [(300, 35, 8, 16), (300, 33, 8, 13), (300, 18, 8, 9), (270, 20, 66, 7), (300, 40, 5, 24), (300, 20, 8, 30), (300, 20, 8, 2)])
+def test_many_short_sequences(B, N, C, S, dtype):
+    """More sequences than compute units: one piece each, from the caller's states on, and four states a wave where few sequences have two."""
+    assert la.la_selective_workspace_bytes(B, N, C, S, 1, 0) == 0
+    lengths = torch.randint(-1, N + 2, (B,), generator=torch.Generator().manual_seed(B + S), dtype=torch.int32)
+    ins = draw(B, N, C, S, 1, dtype, "softplus", S)
+    check(*ins, lengths, "softplus")
+    check(*ins, None, "softplus")
+
+
+def serving_calls(native, monkeypatch):
+    """What the calls of a serving program write, every optional argument there and missing."""
+    out = []
+    with monkeypatch.context() as m:
+        if not native:
+            m.setattr(binding, "_native", None)
+        bf = torch.bfloat16
+        x, w, b, n = rand(2, 20, 40, dtype=bf), rand(40, 4, seed=1), rand(40, seed=2), torch.tensor([20, 7], dtype=torch.int32, device="cuda")
+        A, B, D = -torch.exp(rand(40, 6, seed=4)), rand(2, 20, 2, 6, seed=5, dtype=bf), rand(40, seed=6)
+        ws = room(max(256, la.la_selective_workspace_bytes(2, 20, 40, 6, 2, 0)))
+        for full in (False, True):
+            y, last = poison(2, 20, 40, dtype=bf), poison(2, 3, 40, dtype=bf) if full else None
+            state = rand(2, 3, 40, seed=3, dtype=bf)
+            la.la_conv_forward(x, w, b if full else None, state if full else None, y, last, n if full else None, la.LA_ACT_SILU)
+            token = poison(2, 2, 40, dtype=bf)
+            la.la_conv_step(x[:, :2].contiguous(), w, b if full else None, state, token, la.LA_ACT_NONE if full else la.LA_ACT_SILU)
+            out += [y, last, state, token]
+            y, last, h = poison(2, 20, 40, dtype=bf), poison(2, 40, 6) if full else None, rand(2, 40, 6, seed=7)
+            la.la_selective_forward(x, x, A, B, B, D if full else None, b if full else None, h if full else None, y, last, None, n if full else None,
+                                    la.LA_STEP_SOFTPLUS, ws)
+            token = poison(2, 3, 40, dtype=bf)
+            part, B3 = x[:, :3].contiguous(), B[:, :3].contiguous()
+            la.la_selective_step(part, part, A, B3, B3, D if full else None, b if full else None, h, token,
+                                 la.LA_STEP_SOFTPLUS if full else la.LA_STEP_VALUE)
+            out += [y, last, h, token]
+    return out
+
+
+def test_native_calls_write_what_calls_from_python_write(monkeypatch):
+    la.load_library()
+    assert binding._native is not None
+    native, python = serving_calls(True, monkeypatch), serving_calls(False, monkeypatch)
+    for k, (a, c) in enumerate(zip(native, python)):
+        assert (a is None) == (c is None) and (a is None or (torch.equal(a, c) and torch.isfinite(a).all())), k
+
+
+def test_native_refusals_in_the_words_of_python(monkeypatch):
+    la.load_library()
+    x, w, A, B, D = rand(4, 8, 16), rand(16, 4), rand(16, 5), rand(4, 8, 5), rand(16)
+    none = torch.zeros((), device="cuda")
+
+    def said():
+        words = []
+        for bad in (lambda: la.causal_conv(x, w[:3]), lambda: la.causal_conv(x, w, D[:2]), lambda: la.causal_conv(x, w, D, x), lambda: la.causal_conv(x, w, lengths=D),
+                    lambda: la.causal_conv(x, w[:, :1]), lambda: la.causal_conv(x.half(), w), lambda: la.causal_conv(none, w), lambda: la.causal_conv(x, none),
+                    lambda: la.selective_scan(x, x[:2], A, B, B), lambda: la.selective_scan(x, none, A, B, B), lambda: la.selective_scan(x, x, A, B, none),
+                    lambda: la.selective_scan(x, x, A.half(), B, B), lambda: la.selective_scan(x, x, A, B, B, D, None, D),
+                    lambda: la.la_conv_step(x, w, None, x, x, 1), lambda: la.la_conv_step(x, w, None, D, x, 1),
+                    lambda: la.la_selective_step(x, x, A, B, B, None, None, D, x, 1), lambda: la.la_selective_step(x, x, A, B, B, D, None, rand(4, 16, 5), x[:2], 1),
+                    lambda: la.la_selective_step(x, none, A, B, B, None, None, rand(4, 16, 5), x, 1)):
+            with pytest.raises((ValueError, TypeError, la.LaError)) as e:
+                bad()
+            words.append("%s: %s" % (type(e.value).__name__, e.value))
+        return words
+    native = said()
+    with monkeypatch.context() as m:
+        m.setattr(binding, "_native", None)
+        assert said() == native
