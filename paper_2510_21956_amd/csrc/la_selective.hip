@@ -228,9 +228,10 @@ __device__ __forceinline__ void decays(const Scan &a, const Spot &p, int wave, f
 }
 // v, or 0 where the mask is 0, also of an infinity.
 __device__ __forceinline__ float held(float v, uint32_t mask) { return __uint_as_float(__float_as_uint(v) & mask); }
-// Which of a wave's places hold a state: the others have B = 0 and C = 0, and what would be an infinity times these is taken out.
-// FILLED: all do.
-template <int P, bool FILLED>
+// Whether the states fill the waves' places: kAll; kWaves, some waves hold none, and leave zeros; kPlaces, a wave holds fewer than P.  Places
+// without a state have B = 0 and C = 0, and what would be an infinity times these is taken out.
+enum Fill { kAll, kWaves, kPlaces };
+template <int P, Fill FILL>
 struct Places {
     uint32_t mask[P];
     __device__ __forceinline__ Places(const Scan &a, int wave)
@@ -238,7 +239,7 @@ struct Places {
 #pragma unroll
         for (int j = 0; j < P; ++j) mask[j] = wave * P + j < a.S ? 0xffffffffu : 0;
     }
-    __device__ __forceinline__ float of(float v, int j) const { return FILLED ? v : held(v, mask[j]); }
+    __device__ __forceinline__ float of(float v, int j) const { return FILL == kPlaces ? held(v, mask[j]) : v; }
 };
 // The states that the walk starts from: the caller's, or those that k_selective_chain left for the segment.
 template <int P>
@@ -317,7 +318,7 @@ __global__ void __launch_bounds__(256) k_selective_chain(Scan a)
 }
 
 // FULL: outputs.  Else what the segment makes of zero states.
-template <typename T, int P, int W, bool FULL, bool FILLED>
+template <typename T, int P, int W, bool FULL, Fill FILL>
 __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
 {
     constexpr int OWN = (kPairs + W - 1) / W;  // pairs of rows that a wave prepares
@@ -325,7 +326,7 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
     __shared__ float2 ys[FULL ? W : 1][kPairs][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Spot p(a, lane);
-    const Places<P, FILLED> places(a, wave);
+    const Places<P, FILL> places(a, wave);
     float A[P], h[P];
     Span span;
     decays<P>(a, p, wave, A);
@@ -414,6 +415,8 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
             keep_order();
         });
         if (!FULL) span.add(of_tile);
+        if (FULL && FILL != kAll && wave * P >= a.S)
+            for (int q = 0; q < kPairs; ++q) ys[wave][q][lane] = make_float2(0.f, 0.f);
         block_sync();
         if (FULL) {
 #pragma unroll
@@ -488,7 +491,7 @@ __device__ __forceinline__ float4 over_lanes(float (&v)[64])
 // Registers, of as many waves to a SIMD as the attribute says: 168 for three (four or six waves a workgroup spill 16 to 20 bytes a
 // lane, for 170 and two waves they would not); eight waves, of which four to a SIMD would have 128 and spill 136 bytes, run
 // two to a SIMD (4 x 2048 rows of 1024, 32 states, fp32: 280 us, with four 379); 16 waves a workgroup can't have more than 128.
-template <typename T, int P, int W, bool FULL, bool FILLED>
+template <typename T, int P, int W, bool FULL, Fill FILL>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FULL || W == 16 ? 4 : W == 8 ? 2 : 3))) k_selective_back(Scan a)
 {
     constexpr int OWN = (kPairs + W - 1) / W, PART = kCells / P, PARTS = kRows / PART;
@@ -497,7 +500,7 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
     __shared__ float4 gs[FULL ? W : 1][kPairs][64];
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / 64), lane = threadIdx.x % 64;
     const Spot p(a, lane);
-    const Places<P, FILLED> places(a, wave);
+    const Places<P, FILL> places(a, wave);
     float A[P], carry[P], dA[P], before[P], dD = 0.f, db = 0.f;
     Span span;
     decays<P>(a, p, wave, A);
@@ -636,6 +639,8 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
                     *(float4 *)(shares + part * 64 + (lane & 8) * 4 + (lane & 4) * 4 + (lane & 32) / 4 + (lane & 16) / 4) = sum;
             });
             shares -= W * PARTS * 64;
+            if (FILL != kAll && wave * P >= a.S)
+                for (int q = 0; q < kPairs; ++q) gs[wave][q][lane] = make_float4(0.f, 0.f, 0.f, 0.f);
         } else {
             float of_tile = 0.f;
             each<kPairs>([&](auto q_) {
@@ -891,6 +896,15 @@ void by_shape(const Shape &s, F f)
     with(eight, std::integral_constant<int, 16>());
 }
 
+// f(how S states fill W waves of P as a constant)
+template <int P, int W, typename F>
+void by_fill(int S, F f)
+{
+    if (S == P * W) f(std::integral_constant<Fill, kAll>());
+    else if (S % P) f(std::integral_constant<Fill, kPlaces>());
+    else if constexpr (W > 2) f(std::integral_constant<Fill, kWaves>());  // (one wave or two hold a state each: shape_of)
+}
+
 la_status check_shape(int B, int N, int C, int S, int G)
 {
     if (B < 1 || N < 1 || C < 1 || S < 1 || G < 1 || N > 1 << 30 || S > kMostStates || C % G) return LA_ERR_SHAPE;
@@ -1052,12 +1066,11 @@ la_status la_selective_forward(const void *X, size_t x_stride, const void *Dt, s
         constexpr int p = decltype(P)::value, w = decltype(W)::value;
         if constexpr (p > 2 || w <= 4) {  // (else two states a wave of one piece: lay_out)
             if (a.segs > 1) {
-                la::k_selective<T, p, w, false, true><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective<T, p, w, false, la::kAll><<<grid, dim3(64 * w), 0, st>>>(a);
                 la::k_selective_chain<false><<<chain, dim3(256), 0, st>>>(a);
             }
         }
-        if (S == p * w) la::k_selective<T, p, w, true, true><<<grid, dim3(64 * w), 0, st>>>(a);
-        else la::k_selective<T, p, w, true, false><<<grid, dim3(64 * w), 0, st>>>(a);
+        la::by_fill<p, w>(S, [&](auto F) { la::k_selective<T, p, w, true, decltype(F)::value><<<grid, dim3(64 * w), 0, st>>>(a); });
     };
     la::by_shape<false>(shape, [&](auto P, auto W) {
         if (dt == LA_F32) run((float *)nullptr, P, W);
@@ -1104,12 +1117,11 @@ la_status la_selective_backward(const void *X, size_t x_stride, const void *Dt, 
         constexpr int p = decltype(P)::value, w = decltype(W)::value;
         if constexpr (p > 2 || w <= 4) {
             if (a.segs > 1) {
-                la::k_selective_back<T, p, w, false, true><<<grid, dim3(64 * w), 0, st>>>(a);
+                la::k_selective_back<T, p, w, false, la::kAll><<<grid, dim3(64 * w), 0, st>>>(a);
                 la::k_selective_chain<true><<<chain, dim3(256), 0, st>>>(a);
             }
         }
-        if (S == p * w) la::k_selective_back<T, p, w, true, true><<<grid, dim3(64 * w), 0, st>>>(a);
-        else la::k_selective_back<T, p, w, true, false><<<grid, dim3(64 * w), 0, st>>>(a);
+        la::by_fill<p, w>(S, [&](auto F) { la::k_selective_back<T, p, w, true, decltype(F)::value><<<grid, dim3(64 * w), 0, st>>>(a); });
     };
     la::by_shape<true>(shape, [&](auto P, auto W) {
         if (dt == LA_F32) run((float *)nullptr, P, W);
