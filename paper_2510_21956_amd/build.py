@@ -5,7 +5,9 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
 import warnings
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -29,11 +31,20 @@ def sources():
 
 
 def build_library(verbose=False, extra_flags=(), out=LIB):
-    """Always recompiles; returns the path of the shared library."""
-    cmd = [HIPCC] + FLAGS + list(extra_flags) + ["-I", INCLUDE, "-I", CSRC] + sources() + ["-o", out]
-    if verbose:
-        print(" ".join(cmd))
-    subprocess.run(cmd, check=True)
+    """Always recompiles, the sources side by side (one of them takes a third of the time of all); returns the path of the shared
+    library."""
+    flags = FLAGS + list(extra_flags) + ["-I", INCLUDE, "-I", CSRC]
+
+    def run(cmd):
+        if verbose:
+            print(" ".join(cmd))
+        subprocess.run(cmd, check=True)
+
+    with tempfile.TemporaryDirectory() as folder:
+        objects = {s: os.path.join(folder, os.path.basename(s) + ".o") for s in sources()}
+        with ThreadPoolExecutor(min(8, os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda s: run([HIPCC] + flags + ["-c", s, "-o", objects[s]]), objects))
+        run([HIPCC] + flags + list(objects.values()) + ["-o", out])
     return out
 
 
