@@ -591,7 +591,8 @@ LA_API la_status la_conv_step(const void *X, size_t x_stride, const void *Wt, co
  *       `last` is the state before them (a length of 0 or less leaves h0, one of N or more is N).
  *   workspace: at least la_selective_workspace_bytes(B, N, C, S, G, is_backward) bytes, 256-byte aligned; NULL where that is 0.
  *       Nothing in it has to start at zero.  Calls that share one must not overlap in time, two captured graphs' neither.
- * States, products and sums are float32, the sums in a fixed order: two runs give the same bits.  Addresses are those of elements.
+ * States, products and sums are float32, the sums in a fixed order: two runs give the same bits.  Infinities and NaN go where the
+ * formulas take them, a decay that is too small for a float being 0.  Addresses are those of elements.
  * Limits: B, N, C, S, G >= 1, N <= 2^30, S <= 128, C a multiple of G, every stride, C and G * S < 2^24, B * N * stride < 2^40
  * for every tensor, B * G * ceil(C / G / 64) * ceil(N / 16) < 2^31 and, without the last factor, < 2^21.
  *

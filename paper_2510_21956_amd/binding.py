@@ -1017,7 +1017,7 @@ def la_selective_step(x, dt, A, Bm, Cm, D, bias, state, y, step, stream=None):
 
 
 def in_native_code(name, where, *args):
-    """The result of one of the native functions of csrc/la_bind_layer.cpp; None where there is none, or what it is
+    """The result of one of the native functions of csrc/la_bind_layer.cpp and la_bind_scan.cpp; None where there is none, or what it is
     given is left to the Python code."""
     if _native is None:
         load_library()

@@ -15,7 +15,7 @@
 // Bound by the vector ALU: a state and row of 64 channels takes 21 cycles of a SIMD forward (an exponential 7, two products, a
 // sum, the read-out; reading another lane's value doubles an instruction's time) and 65 backward (states one and a half times, eight operations,
 // sums over the channels 16 to 19).  8 x 2048 rows of 2048 channels, 16 states, bf16: 82 and 254 us of that at 2.1 GHz, 105 us of bytes,
-// 222 and 485 measured (there are 256 chains, two waves to a SIMD); 64 x 512 rows, 164 and 508, 257 and 775.
+// 220 and 470 measured (there are 256 chains, two waves to a SIMD); 64 x 512 rows, 164 and 508, 265 and 769.
 #include "la_checks.h"
 #include "la_common.h"
 #include "la_scalar.h"
@@ -446,9 +446,9 @@ __global__ void __launch_bounds__(64 * W) k_selective(Scan a)
 }
 
 // 64 values a lane, added up over the wave's lanes.  At every step a lane keeps half of its values, by a bit of its
-// number, and adds the partner's share of them, so that 64 sums take a lane 63 additions and not 6 each.  First the partners
+// number, and adds the partner's share of them, so that 64 sums take a lane 116 additions and not 6 each.  First the partners
 // within 16 lanes (rotated by 8, mirrored in 8), whose shares the additions read in place, the kept half chosen by
-// the instruction's mask of banks; then halves and quarters of the wave change places, one instruction for two values; the
+// the instruction's mask of banks, two additions a value; then halves and quarters of the wave change places, one instruction for two values; the
 // last four values are added up over four neighbours.  Lane l ends with values 32 l3 + 16 l2 + 8 l5 + 4 l4 + (0 .. 3), l3 being bit 3
 // of l.  An instruction that reads another lane's register needs two others behind the one that wrote it.
 #define LA_FOLD(to, from, how, banks) "v_add_f32_dpp " to ", " to ", " to " " how " row_mask:0xf bank_mask:0xf\n\t" \
@@ -488,9 +488,10 @@ __device__ __forceinline__ float4 over_lanes(float (&v)[64])
 
 // Backward.  FULL: outputs, walking the tiles from the far end: states from the saved ones before the tile on, then the rows in
 // reverse.  Else what the segment hands to the rows before it from nothing behind it.
-// Registers, of as many waves to a SIMD as the attribute says: 168 for three (four or six waves a workgroup spill 16 to 20 bytes a
-// lane, for 170 and two waves they would not); eight waves, of which four to a SIMD would have 128 and spill 136 bytes, run
-// two to a SIMD (4 x 2048 rows of 1024, 32 states, fp32: 280 us, with four 379); 16 waves a workgroup can't have more than 128.
+// Registers, of as many waves to a SIMD as the attribute says: 168 for three (two, four and six waves a workgroup spill 12 to 20 bytes a
+// lane, for 170 and two waves to a SIMD they would not; twelve waves of eight states 184); eight waves, of which four to a SIMD would have 128 and spill 136 bytes, run
+// two to a SIMD (4 x 2048 rows of 1024, 32 states, fp32: 280 us, with four 379); 16 waves a workgroup can't have more than 128 (380 bytes
+// of spills).
 template <typename T, int P, int W, bool FULL, Fill FILL>
 __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FULL || W == 16 ? 4 : W == 8 ? 2 : 3))) k_selective_back(Scan a)
 {
@@ -948,7 +949,10 @@ struct Inputs {
 // the walk along the segments).  512 rows take, in us, with w waves on every SIMD of the busiest compute units (S = 16, bf16):
 // 39 + 29 w forward (31 + 35 w with two states a wave), 100 + 80 w backward (5 + 117 w), what the segments make of zero states 28 + 23 w and 31 + 21 w.  Segments fill the
 // compute units once forward, about twice backward (5 waves to a SIMD at once, backward 2 to 4), and have 32 rows at least; one
-// piece where that takes less.  Of 1 to 96 segments, on 10 shapes of 1 to 256 chains, this takes 1.04 times the best on the average.
+// piece where that takes less.  Of 1 to 96 segments, on 10 shapes of 1 to 256 chains, this takes 1.04 times the best on the average.  The
+// constants are those of 16 states; of 1 to 128 segments, on 5 shapes of 8 to 512 chains, other numbers of states take, forward and backward, 1.11
+// and 1.14 times the best with 4 (at most 1.4: one sequence of 8192 rows), 1.02 and 1.07 with 8, 1.07 and 1.02 with 24, 1.02 and 1.01 with 32,
+// 1.00 and 1.01 at most with 64, 100 and 128.
 // One piece and few waves: two states a wave instead of four, whose twice as many waves hide each other's
 // waits (8 x 2048 rows of 2048 channels 222 us forward, with four 260, in 8 segments 240; backward 484, in 3 segments
 // 546; with 12 states backward 543 and 529: only from 13 on).
