@@ -853,6 +853,14 @@ def _strided(ref, dims=1, **ts):
     return out
 
 
+def _choice(name, x):
+    """x as the library's int."""
+    x = int(x)
+    if not -_INTS <= x < _INTS:  # ctypes would cut it off
+        raise ValueError("%s is none of its constants: %d" % (name, x))
+    return x
+
+
 def _natively(name, where, *args):
     """Whether the call was made in native code (csrc/la_bind_scan.cpp)."""
     if _native is None:
@@ -899,7 +907,7 @@ def la_conv_forward(x, weight, bias, state, y, last, lengths, act, stream=None):
     _needed(x=x, weight=weight, y=y)
     stride, sizes, codes = _conv(x, weight, bias, y, lengths, state=state, last=last)
     _call("la_conv_forward", x, stream, (y, last), _ptr(x), stride, _ptr(weight), _ptr(bias), _ptr(state), _ptr(y), _ptr(last),
-          _lengths_ptr(lengths, x), *sizes, int(act), *codes)
+          _lengths_ptr(lengths, x), *sizes, _choice("act", act), *codes)
 
 
 def la_conv_backward(x, weight, bias, state, dy, dlast, dx, dweight, dbias, dstate, lengths, act, workspace, stream=None):
@@ -914,7 +922,7 @@ def la_conv_backward(x, weight, bias, state, dy, dlast, dx, dweight, dbias, dsta
         if t is not None and (t.shape != shape or t.dtype != torch.float32):
             raise ValueError("%s must be float32 %s" % (name, tuple(shape)))
     _call("la_conv_backward", x, stream, (dx, dweight, dbias, dstate), _ptr(x), stride, _ptr(weight), _ptr(bias), _ptr(state),
-          _ptr(dy), _ptr(dlast), _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(dstate), _lengths_ptr(lengths, x), *sizes, int(act),
+          _ptr(dy), _ptr(dlast), _ptr(dx), _ptr(dweight), _ptr(dbias), _ptr(dstate), _lengths_ptr(lengths, x), *sizes, _choice("act", act),
           *codes, *_room(workspace))
 
 
@@ -925,7 +933,7 @@ def la_conv_step(x, weight, bias, state, y, act, stream=None):
         return
     _needed(x=x, weight=weight, state=state, y=y)
     stride, sizes, codes = _conv(x, weight, bias, y, None, state=state)
-    _call("la_conv_step", x, stream, (y, state), _ptr(x), stride, _ptr(weight), _ptr(bias), _ptr(state), _ptr(y), *sizes, int(act),
+    _call("la_conv_step", x, stream, (y, state), _ptr(x), stride, _ptr(weight), _ptr(bias), _ptr(state), _ptr(y), *sizes, _choice("act", act),
           *codes)
 
 
@@ -984,7 +992,7 @@ def la_selective_forward(x, dt, A, Bm, Cm, D, bias, h0, y, last, saved, lengths,
     head, sizes = _selective(x, dt, A, Bm, Cm, D, bias, lengths, {"h0": h0, "last": last}, {"y": y})
     _check_tensors(A, saved, workspace)
     _call("la_selective_forward", x, stream, (y, last, saved), *head, _ptr(h0), _ptr(y), _ptr(last), *_room(saved),
-          _lengths_ptr(lengths, x), *sizes, int(step), _real_code(x), *_room(workspace))
+          _lengths_ptr(lengths, x), *sizes, _choice("step", step), _real_code(x), *_room(workspace))
 
 
 def la_selective_backward(x, dt, A, Bm, Cm, D, bias, saved, dy, dlast, dx, ddt, dA, dB, dC, dD, dbias, dh0, lengths, step, workspace,
@@ -1001,7 +1009,7 @@ def la_selective_backward(x, dt, A, Bm, Cm, D, bias, saved, dy, dlast, dx, ddt, 
             raise ValueError("%s must be float32 [%d]" % (name, A.shape[0]))
     _call("la_selective_backward", x, stream, (dx, ddt, dA, dB, dC, dD, dbias, dh0), *head, *_room(saved), _ptr(dy), _ptr(dlast),
           _ptr(dx), _ptr(ddt), _ptr(dA), _ptr(dB), _ptr(dC), _ptr(dD), _ptr(dbias), _ptr(dh0), _lengths_ptr(lengths, x), *sizes,
-          int(step), _real_code(x), *_room(workspace))
+          _choice("step", step), _real_code(x), *_room(workspace))
 
 
 def la_selective_step(x, dt, A, Bm, Cm, D, bias, state, y, step, stream=None):
@@ -1013,7 +1021,7 @@ def la_selective_step(x, dt, A, Bm, Cm, D, bias, state, y, step, stream=None):
     dims = 1 if Bm.dim() == x.dim() else 2
     x, dt, Bm, Cm = _near(x, 1, stream), _near(dt, 1, stream), _near(Bm, dims, stream), _near(Cm, dims, stream)
     head, sizes = _selective(x, dt, A, Bm, Cm, D, bias, None, {"state": state}, {"y": y})
-    _call("la_selective_step", x, stream, (y, state), *head, _ptr(state), _ptr(y), *sizes, int(step), _real_code(x))
+    _call("la_selective_step", x, stream, (y, state), *head, _ptr(state), _ptr(y), *sizes, _choice("step", step), _real_code(x))
 
 
 def in_native_code(name, where, *args):

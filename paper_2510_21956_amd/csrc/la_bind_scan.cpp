@@ -51,6 +51,13 @@ bool rows_fit(const at::Tensor &t, const at::Tensor &ref, int dims, at::IntArray
     return t.defined() && t.is_cuda() && !t.unsafeGetTensorImpl()->is_python_dispatch() && t.get_device() == ref.get_device() &&
            t.scalar_type() == ref.scalar_type() && t.sizes() == sizes && row_stride(t, dims);
 }
+// An int that is one of the library's constants, or that it refuses; a larger one is the Python function's to refuse.
+int choice(PyObject *o)
+{
+    const long x = PyLong_AsLong(o);
+    require(x == (int)x && !(x == -1 && PyErr_Occurred()));
+    return (int)x;
+}
 la_dtype code_of(const at::Tensor &t) { return t.scalar_type() == at::kFloat ? LA_F32 : LA_BF16; }
 // The sizes of x but for its last `but` dimensions, and more.
 std::vector<int64_t> leading(const at::Tensor &x, int but, std::initializer_list<int64_t> more)
@@ -185,7 +192,7 @@ PyObject *conv_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const size_t stride = row_stride(x, 1);
         require(stride);
         const ConvSizes s(x, w);
-        const la_act act = (la_act)PyLong_AsLong(a[7]);
+        const la_act act = (la_act)choice(a[7]);
         void *const st = stream_of(a[8], x), *p[7];
         for (int i = 0; i < 7; ++i) p[i] = address(a[i]);
         const c10::DeviceGuard guard(x.device());
@@ -210,7 +217,7 @@ PyObject *conv_step(PyObject *, PyObject *const *a, Py_ssize_t n)
         const size_t stride = row_stride(x, 1);
         require(stride);
         const ConvSizes s(x, w);
-        const la_act act = (la_act)PyLong_AsLong(a[5]);
+        const la_act act = (la_act)choice(a[5]);
         void *const st = stream_of(a[6], x), *p[5];
         for (int i = 0; i < 5; ++i) p[i] = address(a[i]);
         const c10::DeviceGuard guard(x.device());
@@ -387,7 +394,7 @@ PyObject *scan_forward(PyObject *, PyObject *const *a, Py_ssize_t n)
         const ScanCall c(a, a[11]);
         check_scan(a, a[9], a[11]);
         check_packed({a[2], a[9], a[10], a[13]});
-        const la_step step = (la_step)PyLong_AsLong(a[12]);
+        const la_step step = (la_step)choice(a[12]);
         void *const st = stream_of(a[14], c.x), *p[14];
         for (int i = 0; i < 14; ++i) p[i] = i == 12 ? nullptr : address(a[i]);
         const size_t sb = is_none(a[10]) ? 0 : bytes(tensor(a[10])), wb = is_none(a[13]) ? 0 : bytes(tensor(a[13]));
@@ -411,7 +418,7 @@ PyObject *scan_step(PyObject *, PyObject *const *a, Py_ssize_t n)
             if (is_none(a[i])) Py_RETURN_NONE;
         const ScanCall c(a, Py_None);
         require(std::max({c.xs, c.ts, c.bs, c.cs}) < kRowsApart);  // the Python function copies
-        const la_step step = (la_step)PyLong_AsLong(a[9]);
+        const la_step step = (la_step)choice(a[9]);
         void *const st = stream_of(a[10], c.x), *p[9];
         for (int i = 0; i < 9; ++i) p[i] = address(a[i]);
         const c10::DeviceGuard guard(c.x.device());

@@ -289,3 +289,15 @@ def test_native_refusals_in_the_words_of_python(monkeypatch):
     with monkeypatch.context() as m:
         m.setattr(binding, "_native", None)
         assert said() == native
+
+
+def test_constants_beyond_32_bits_in_native_code():
+    x, w, y = rand(2, 8, 16), rand(16, 4), poison(2, 8, 16)
+    A, B, h = rand(16, 4), rand(2, 8, 4), rand(2, 16, 4)
+    for value in ((1 << 32) + 1, 1 << 70):
+        for call in (lambda: la.la_conv_forward(x, w, None, None, y, None, None, value), lambda: la.la_conv_step(x, w, None, rand(2, 3, 16), y, value),
+                     lambda: la.la_selective_forward(x, x, A, B, B, None, None, None, y, None, None, None, value, None),
+                     lambda: la.la_selective_step(x, x, A, B, B, None, None, h, y, value)):
+            with pytest.raises(ValueError, match="constants"):
+                call()
+    assert y.isnan().all()

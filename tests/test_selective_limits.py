@@ -113,3 +113,19 @@ def test_other_lanes_registers_are_waited_for(tmp_path):
             for r in [*_registers(operands[0]), *(_registers(operands[1]) if swap else ())]:
                 written[r] = now
     assert seen > 10000
+
+
+@pytest.mark.parametrize("value", [1 << 32, (1 << 32) + 1, -(1 << 40), 1 << 70])
+def test_constants_beyond_32_bits_are_refused(value):
+    """What a C int would cut off to a constant that there is."""
+    D = lambda *s, t=torch.bfloat16: _stand_in(torch.zeros(*s, dtype=t))  # noqa: E731
+    F = torch.float32
+    x, y, w, A, B, h = D(2, 8, 16), D(2, 8, 16), D(16, 4, t=F), D(16, 4, t=F), D(2, 8, 4), D(2, 16, 4, t=F)
+    for call in (lambda: la.la_conv_forward(x, w, None, None, y, None, None, value), lambda: la.la_conv_step(x, w, None, D(2, 3, 16), y, value),
+                 lambda: la.la_conv_backward(x, w, None, None, y, None, D(2, 8, 16), None, None, None, None, value, None),
+                 lambda: la.la_selective_forward(x, x, A, B, B, None, None, None, y, None, None, None, value, None),
+                 lambda: la.la_selective_backward(x, x, A, B, B, None, None, D(1 << 16, t=torch.uint8), y, None, *(D(2, 8, 16) for _ in range(2)), None, D(2, 8, 4),
+                                                  D(2, 8, 4), None, None, None, None, value, None),
+                 lambda: la.la_selective_step(x, x, A, B, B, None, None, h, y, value)):
+        with pytest.raises(ValueError, match="constants"):
+            call()
