@@ -581,11 +581,12 @@ __global__ void __launch_bounds__(64 * W) __attribute__((amdgpu_waves_per_eu(!FU
                     const float4 s = du[q][lane];
                     each<2 * P>([&](auto i) {
                         constexpr int r = decltype(i)::value / P, j = decltype(i)::value % P, k = (2 * q + r) * P + j;
-                        const float u = places.of(r ? s.w : s.y, j);
-                        h0[j] = fmaf(__builtin_amdgcn_exp2f((r ? s.z : s.x) * A[j]), h0[j], u * of_lane<k % 16>(B.v[k / 16]));
+                        h0[j] = fmaf(__builtin_amdgcn_exp2f((r ? s.z : s.x) * A[j]), h0[j], (r ? s.w : s.y) * of_lane<k % 16>(B.v[k / 16]));
                     });
                     if (q % 2) keep_order();
                 });
+#pragma unroll
+                for (int j = 0; j < P; ++j) h0[j] = places.of(h0[j], j);
                 float4 s = du[first][lane];
                 each<PART / 2>([&](auto q_) {
                     constexpr int q = decltype(q_)::value;
